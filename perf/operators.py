@@ -190,7 +190,7 @@ def _pool(s):
     from paper_2604_26968_b200 import workloads as W
     c = s["case"]
     if c["kind"] == "evict":
-        part = W.gqa(1, c["heads"], c["heads"], 1, 16, s["blocks"], 16)
+        part = W.gqa(1, c["heads"], c["heads"], 1, 16, s["blocks"], max(16, s["n"] - s["resident"]))
     elif c["arch"] == "mla":
         part = W.mla(LAYERS, c["dim"], c["rope"], c["block"], s["blocks"], 16)
     else:
@@ -198,13 +198,16 @@ def _pool(s):
         part = make(LAYERS, c["q_heads"], c["heads"], c["dim"], c["block"], s["blocks"], 16)
     pool = B.Pool([part], n_tags=part.n_entries, staging_bytes=max(1 << 20, 2 * part.entry_bytes + 4096), max_promote=16,
                   host_meta=False, stream=torch.cuda.current_stream())
-    pairs = torch.zeros(s["resident"], dtype=torch.uint8, device="cuda")
+    pairs = torch.zeros(part.n_entries, dtype=torch.uint8, device="cuda")
     rc, n = pool.kv_admit(0, 0.9, pairs, False)
-    if rc or n != s["resident"]:
+    if rc or n != part.n_entries:
         raise RuntimeError("kv_admit: %d, %d" % (rc, n))
     if c["kind"] == "evict":
-        pool.tag[: len(s["tag"])] = s["tag"]
-        pool.last_epoch[: len(s["tag"])] = s["last_epoch"]
+        if s["resident"] < s["n"]:      # the free ones have been demoted
+            _ok(pool.kv_demote(torch.arange(s["resident"], s["n"], dtype=torch.int32, device="cuda"), s["n"] - s["resident"], 1 << 19))
+            pool.sync()
+        pool.tag[: s["resident"]] = s["tag"][: s["resident"]]
+        pool.last_epoch[: s["n"]] = s["last_epoch"]
         s["victims"] = torch.empty(max(4, s["k"]), dtype=torch.int32, device="cuda")
     else:
         pool.slabs[0].copy_(s["slab"].view(-1).view(torch.uint8))

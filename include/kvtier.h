@@ -81,6 +81,7 @@ typedef enum { KV_AUTO = -1, KV_MHA = 0, KV_GQA = 1, KV_MQA = 2, KV_MLA = 3 } kv
 #define KV_DEV_WAIT_EXPIRED 32u      /* a bounded wait inside a kernel gave up */
 #define KV_DEV_BAD_HEAD_VALUE 64u    /* a head observation or multiplier was negative or not finite */
 #define KV_DEV_BAD_SPAN_VALUE 128u   /* an attention-span observation was negative or not finite */
+#define KV_DEV_BLOCK_NOT_RESIDENT 256u /* kv_append: a token's block is not in HBM (its K/V were not written) */
 
 typedef struct {
   int32_t variant;    /* kv_variant_t; KV_AUTO infers it from the fields below */
@@ -458,6 +459,129 @@ uint64_t kv_dedup_table_slots(uint64_t m);
 int32_t kv_dedup_digests(const uint8_t* d_digests, uint64_t m, uint32_t* d_canon, uint32_t* d_refcount,
                          uint32_t* d_table, uint64_t table_slots, uint32_t* d_n_unique,
                          uint32_t* d_status, kv_stream_t stream);
+
+/* ---- what a model writes into the cache, and reads from it ------------------------
+ * The calls below work on one layer of one partition whose elements have 16 bits
+ * (kv_model_desc.dtype_bits == 16), through block tables as kv_prefetch_list takes them:
+ * d_table (device, u32 [n_rows][n_layers][KV heads]; one column for MLA) holds handles
+ * (tags); a run of its rows holds the position-blocks of a sequence, or of a prefix that
+ * several share, in order.  A handle leads to its block wherever that is in the partition
+ * (d_loc[handle] = entry).  They are enqueued on `stream` (the pool's compute stream),
+ * which first joins the pool's promotions in flight; nothing of them waits on the host, and
+ * they may be captured into a graph.  q, k, v and outputs may have any strides (elements;
+ * the innermost dimension is contiguous) and the alignment of their elements.  The device
+ * that owns the pool has to be the current one. */
+typedef enum { KV_DTYPE_BF16 = 0, KV_DTYPE_F16 = 1 } kv_dtype_t;
+
+/* Rotary positions.  Elements rot_first .. rot_first + rot_dim - 1 of every head turn in pairs:
+ * pair i is (i, i + rot_dim/2), or (2i, 2i+1) if interleaved, counted from rot_first, and turns by
+ * the angle pos[axis[i]] * d_inv_freq[i] (formed in binary64), so that each pair follows one
+ * of up to four axes of position: text has one, images and video have time, height and
+ * width.  rot_dim is even, 0 (nothing turns) to 256. */
+typedef struct {
+  int32_t rot_dim;
+  int32_t rot_first;
+  int32_t interleaved;
+  int32_t n_axes;          /* 1..4; 0 if rot_dim is 0 */
+  uint8_t axis[128];       /* axis[i] < n_axes, i < rot_dim/2 */
+  const float* d_inv_freq; /* (device) f32 [rot_dim/2] */
+} kv_rope_desc;
+
+/* kv_append: writes the keys and values of n_tokens new tokens into their blocks, keys rotated,
+ * and the rotated queries to d_q_out (which may be d_q itself).  Token t's place is row
+ * d_slot[t] / block_tokens of the table, token d_slot[t] % block_tokens of that block; a token with
+ * d_slot[t] < 0 is padding, and nothing of it is written.  Slots (and the blocks that the
+ * handles of a row name) are distinct: of two tokens with one place, each element is one's or the
+ * other's.  A head whose block is not in HBM is left out and sets KV_DEV_BLOCK_NOT_RESIDENT; a
+ * slot beyond the table sets KV_DEV_BAD_INDEX and nothing of its token is written.
+ * A key head has head_dim elements (MLA: one row of d_latent + d_rope elements, and no values:
+ * d_v is NULL); so has a query head.  Results are rounded once from binary32. */
+typedef struct {
+  int32_t partition, layer;
+  int32_t dtype;           /* kv_dtype_t */
+  int32_t reserved;
+  uint64_t n_tokens;
+  const void* d_k;         /* (device) [n_tokens][KV heads][dim] */
+  int64_t k_stride[2];     /* token, head */
+  const void* d_v;
+  int64_t v_stride[2];
+  const void* d_q;         /* [n_tokens][query heads][dim], or NULL: keys and values alone */
+  int64_t q_stride[2];
+  void* d_q_out;
+  int64_t q_out_stride[2];
+  const uint32_t* d_table;
+  uint64_t n_rows;
+  const int64_t* d_slot;   /* (device) [n_tokens] */
+  const int32_t* d_pos;    /* (device) [n_axes][n_tokens]; NULL if rot_dim is 0 */
+  kv_rope_desc rope;
+} kv_append_desc;
+int32_t kv_append(kv_pool* pool, const kv_append_desc* desc, kv_stream_t stream);
+
+/* kv_attend: attention of one query token per sequence,
+ *   out[s][j] = sum_t p_t v_t,  p_t = exp(scale * q[s][j].k_t - lse[s][j]),
+ *   lse[s][j] = log sum_t exp(scale * q[s][j].k_t)
+ * over the tokens of its group's prefix, if it is in a group, and of its suffix; query head j reads
+ * KV head j / (query heads / KV heads) (MLA: all read the one row, the first d_latent elements
+ * of which are the value).  The prefix of a group is read once for all its sequences.
+ *   d_suffix  (device, u32 [n_seqs][2])   first table row and tokens of each sequence's own run
+ *   d_prefix  (device, u32 [n_groups][2]) the same of each group's shared run
+ *   d_group   (device, u32 [n_groups+1])  sequences d_group[g] .. d_group[g+1]-1 are group g's;
+ *             ascending; sequences outside have no prefix.  n_groups may be 0.
+ * Runs may overlap and lengths may be 0.  (Several new tokens of a sequence -- drafts to be checked --
+ * are as many sequences, one group whose prefix is what lies before them, their suffixes one run of
+ * different lengths.)  Blocks that are not in HBM -- demoted, dropped, handles that name nothing --
+ * are passed over, and so is what lies in a block behind a run's last token, whatever it holds.
+ * A sequence with nothing to attend to gets zeros and lse = -inf.  Scores, their sums and the
+ * outputs are binary32 until out is rounded; the probabilities enter the product with the
+ * values in the elements' type.
+ * max_suffix, max_prefix (tokens) and max_members (sequences of a group) bound what the arrays hold:
+ * the arrays may change between replays of a captured call, the bounds may not.  A run or group
+ * beyond them or beyond the table counts as empty and sets KV_DEV_BAD_INDEX.  max_prefix == 0 or
+ * max_members == 0: no prefix is looked at.
+ * d_weight (device, u64 [n_tags], optional): the attention weight p_t of every query head and sequence,
+ * summed over the tokens of a block, is added to d_weight[handle], in units of 2^-32 (rounded; integer
+ * sums, so that the result does not depend on an order): what kv_attention_score takes.
+ * d_scratch (device, 16-byte aligned): kv_attend_scratch_bytes of the same partition and bounds; two calls
+ * that may run at the same time need two.  Same results on every run.
+ * head_dim is a multiple of 8 up to 256; MLA: d_latent up to 512 and d_latent + d_rope up to 576, multiples
+ * of 8; else KV_ERR_UNSUPPORTED_VARIANT. */
+typedef struct {
+  int32_t partition, layer;
+  int32_t dtype;           /* kv_dtype_t */
+  float scale;
+  uint32_t n_seqs, n_groups;
+  uint32_t max_suffix, max_prefix, max_members;
+  uint32_t reserved;
+  const void* d_q;         /* (device) [n_seqs][query heads][dim] */
+  int64_t q_stride[2];     /* sequence, head */
+  void* d_out;             /* (device) [n_seqs][query heads][value dim] */
+  int64_t out_stride[2];
+  float* d_lse;            /* (device, optional) [n_seqs][query heads] */
+  const uint32_t* d_table;
+  uint64_t n_rows;
+  const uint32_t* d_suffix;
+  const uint32_t* d_prefix;
+  const uint32_t* d_group;
+  uint64_t* d_weight;
+  void* d_scratch;
+  uint64_t scratch_bytes;
+} kv_attend_desc;
+int32_t kv_attend(kv_pool* pool, const kv_attend_desc* desc, kv_stream_t stream);
+/* Scratch of a call with these bounds (weights: with d_weight); 0 if kv_attend would refuse them. */
+uint64_t kv_attend_scratch_bytes(kv_pool* pool, int32_t partition, uint32_t n_seqs, uint32_t n_groups,
+                                 uint32_t max_suffix, uint32_t max_prefix, uint32_t max_members, int32_t weights);
+
+/* kv_attention_score: eviction by accumulated attention weight.  For every RESIDENT entry, g its
+ * handle (binary32, each operation rounded once):
+ *   d_acc[g] = decay * d_acc[g] + float(d_weight[g]) * 2^-32,  d_weight[g] = 0,
+ *   d_score[entry] = d_acc[g], or +inf if fewer than `protect` epochs lie between the entry's last
+ *                    epoch (its last touch, or its admission) and `epoch`;
+ * FREE entries get +inf.  kv_select_victims (or kv_select_victim_blocks) then chooses the lowest.
+ * d_weight (device, u64 [n_tags]) and d_acc (device, f32 [n_tags]) are zeroed by the caller once; they
+ * belong to handles, so a block keeps what it has gathered while it is in the host tier, where it does not decay.
+ * 0 <= decay <= 1; protect < 2^31.  The pool's predictor, EMA and touches are left alone. */
+int32_t kv_attention_score(kv_pool* pool, uint32_t epoch, float decay, uint32_t protect, uint64_t* d_weight,
+                           float* d_acc, kv_stream_t stream);
 
 /* Block-granular selection (head-granular eviction section: eviction takes the
  * block with the lowest weighted aggregate importance across heads, with head

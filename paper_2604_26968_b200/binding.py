@@ -29,6 +29,8 @@ KV_NONE = 0xFFFFFFFF
 KV_DEV_BAD_INDEX = 16
 KV_DEV_BAD_HEAD_VALUE = 64
 KV_DEV_BAD_SPAN_VALUE = 128
+KV_DEV_BLOCK_NOT_RESIDENT = 256
+KV_DTYPE_BF16, KV_DTYPE_F16 = 0, 1
 KV_LOC_HOST = 0x80000000
 
 
@@ -81,6 +83,34 @@ class kv_slot_meta(C.Structure):
                 ("decay", C.c_float), ("pair", C.c_uint32), ("demote_epoch", C.c_uint32)]
 
 
+class kv_rope_desc(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("rot_first", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32),
+                ("axis", C.c_uint8 * 128), ("d_inv_freq", C.c_void_p)]
+
+
+_stride = C.c_int64 * 2
+
+
+class kv_append_desc(C.Structure):
+    _fields_ = [("partition", C.c_int32), ("layer", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32),
+                ("n_tokens", C.c_uint64),
+                ("d_k", C.c_void_p), ("k_stride", _stride), ("d_v", C.c_void_p), ("v_stride", _stride),
+                ("d_q", C.c_void_p), ("q_stride", _stride), ("d_q_out", C.c_void_p), ("q_out_stride", _stride),
+                ("d_table", C.c_void_p), ("n_rows", C.c_uint64), ("d_slot", C.c_void_p), ("d_pos", C.c_void_p),
+                ("rope", kv_rope_desc)]
+
+
+class kv_attend_desc(C.Structure):
+    _fields_ = [("partition", C.c_int32), ("layer", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("n_seqs", C.c_uint32), ("n_groups", C.c_uint32),
+                ("max_suffix", C.c_uint32), ("max_prefix", C.c_uint32), ("max_members", C.c_uint32),
+                ("reserved", C.c_uint32),
+                ("d_q", C.c_void_p), ("q_stride", _stride), ("d_out", C.c_void_p), ("out_stride", _stride),
+                ("d_lse", C.c_void_p), ("d_table", C.c_void_p), ("n_rows", C.c_uint64),
+                ("d_suffix", C.c_void_p), ("d_prefix", C.c_void_p), ("d_group", C.c_void_p),
+                ("d_weight", C.c_void_p), ("d_scratch", C.c_void_p), ("scratch_bytes", C.c_uint64)]
+
+
 SLOT_META_DTYPE = np.dtype([("tag", "<u4"), ("last_epoch", "<u4"), ("ema", "<f4"),
                             ("decay", "<f4"), ("pair", "<u4"), ("demote_epoch", "<u4")])
 
@@ -90,6 +120,7 @@ EXPORTS = ("kv_size_bytes", "kv_infer_variant", "kv_entry_bytes", "kv_workspace_
            "kv_promote", "kv_set_deferred_packing", "kv_flush", "kv_max_batch_bytes", "kv_admit", "kv_get_stats", "kv_ring_query",
            "kv_last_demote_counts", "kv_device_status", "kv_timing_enable", "kv_timing_read",
            "kv_set_select_variant", "kv_selection_stats", "kv_demote_counted", "kv_victim_counts", "kv_set_gather_threshold", "kv_set_l2_residency", "kv_last_cuda_error", "kv_status_string",
+           "kv_append", "kv_attend", "kv_attend_scratch_bytes", "kv_attention_score",
            "kv_version")
 
 _lib = None
@@ -201,6 +232,14 @@ def load():
     L.kv_set_gather_threshold.argtypes = [vp, u64]
     L.kv_selection_stats.restype = i32
     L.kv_selection_stats.argtypes = [vp, vp, vp]
+    L.kv_append.restype = i32
+    L.kv_append.argtypes = [vp, C.POINTER(kv_append_desc), vp]
+    L.kv_attend.restype = i32
+    L.kv_attend.argtypes = [vp, C.POINTER(kv_attend_desc), vp]
+    L.kv_attend_scratch_bytes.restype = u64
+    L.kv_attend_scratch_bytes.argtypes = [vp, i32, u32, u32, u32, u32, u32, i32]
+    L.kv_attention_score.restype = i32
+    L.kv_attention_score.argtypes = [vp, u32, C.c_float, u32, vp, vp, vp]
     L.kv_last_cuda_error.restype = i32
     L.kv_last_cuda_error.argtypes = [vp]
     L.kv_status_string.restype = C.c_char_p
@@ -258,6 +297,34 @@ def kv_select_victims_static(d_score, d_state, n, k, d_victims, d_status=None, s
         d_score.data_ptr(), d_state.data_ptr(), int(n), int(k),
         d_victims.data_ptr() if d_victims is not None else None,
         d_status.data_ptr() if d_status is not None else None, _stream_ptr(stream))
+
+
+class kv_rope:
+    """Rotary positions for kv_append: kv_rope_desc and the tensor it points to.  axis: the axis of
+    position each pair follows (an int for all of them)."""
+
+    def __init__(self, rot_dim, axis, inv_freq, first=0, interleaved=False, n_axes=None):
+        half = int(rot_dim) // 2
+        axis = [int(axis)] * half if isinstance(axis, int) else [int(x) for x in axis]
+        if len(axis) != half or half > 128 or (inv_freq.numel() if inv_freq is not None else 0) < half:
+            raise ValueError("kv_rope: %d axes and %s frequencies for %d pairs" %
+                             (len(axis), inv_freq.numel() if inv_freq is not None else "no", half))
+        self.inv_freq = inv_freq
+        self.n_axes = int(n_axes if n_axes is not None else (max(axis) + 1 if axis else 0))
+        self.desc = kv_rope_desc(int(rot_dim), int(first), int(bool(interleaved)), self.n_axes,
+                                 (C.c_uint8 * 128)(*axis), inv_freq.data_ptr() if inv_freq is not None else None)
+
+
+def _typed(name, tensors, dtypes):
+    for t in tensors:
+        if t is not None and str(t.dtype) not in dtypes:
+            raise TypeError("%s: a tensor of %s where %s is wanted" % (name, t.dtype, " or ".join(dtypes)))
+
+
+def _plain(name, tensors):
+    for t in tensors:
+        if t is not None and not t.is_contiguous():
+            raise ValueError("%s: arrays of indices and results have to be contiguous" % name)
 
 
 class Pool:
@@ -456,6 +523,99 @@ class Pool:
                                          d_out_slots.data_ptr() if d_out_slots is not None else None, int(max_out),
                                          d_out_count.data_ptr() if d_out_count is not None else None,
                                          _stream_ptr(self.compute))
+
+    def _heads_view(self, name, q, t, n, heads, dim, dtype):
+        """(address, strides) of a [n][heads][dim] tensor of 16-bit elements."""
+        if t is None:
+            return None, _stride(0, 0)
+        if str(t.dtype) != dtype or tuple(t.shape) != (n, heads, dim) or (dim > 1 and t.stride(2) != 1):
+            raise ValueError("%s: %s %s where %s (%d, %d, %d) with contiguous rows is wanted" %
+                             (name, t.dtype, tuple(t.shape), dtype, n, heads, dim))
+        return t.data_ptr(), _stride(t.stride(0), t.stride(1))
+
+    def _attention_dims(self, q):
+        """(key heads, elements of a query or key head, of a value head)"""
+        p = self.parts[q]
+        return ((1, p.d_latent + p.d_rope, p.d_latent) if p.variant == KV_MLA else (p.heads, p.head_dim, p.head_dim))
+
+    def _table_rows(self, name, q, table):
+        p = self.parts[q]
+        _typed(name, [table], ("torch.int32", "torch.uint32"))
+        _plain(name, [table])
+        if tuple(table.shape[1:]) != (p.n_layers, p.heads) or table.dim() != 3:
+            raise ValueError("%s: a table of %s where (rows, %d, %d) is wanted" % (name, tuple(table.shape), p.n_layers, p.heads))
+        return table.shape[0]
+
+    def kv_append(self, q, layer, d_k, d_v, d_table, d_slot, d_q=None, d_q_out=None, rope=None, d_pos=None, stream=None):
+        """d_k, d_v, d_q, d_q_out: [tokens, heads, dim] (any strides but the last); d_slot int64 [tokens];
+        d_pos int32 [axes, tokens]; rope: kv_rope."""
+        n = d_slot.numel()
+        H, dk, dv = self._attention_dims(q)
+        dt = str(d_k.dtype)
+        if dt not in ("torch.bfloat16", "torch.float16"):
+            raise TypeError("kv_append: keys of %s" % dt)
+        _typed("kv_append", [d_slot], ("torch.int64",))
+        _typed("kv_append", [d_pos], ("torch.int32",))
+        _plain("kv_append", [d_slot, d_pos])
+        if rope is not None and d_pos is not None and d_pos.numel() != rope.n_axes * n:
+            raise ValueError("kv_append: %d positions for %d axes of %d tokens" % (d_pos.numel(), rope.n_axes, n))
+        QH = self.parts[q].n_q_heads
+        d = kv_append_desc(int(q), int(layer), KV_DTYPE_BF16 if dt == "torch.bfloat16" else KV_DTYPE_F16, 0, n)
+        d.d_k, d.k_stride = self._heads_view("kv_append", q, d_k, n, H, dk, dt)
+        d.d_v, d.v_stride = self._heads_view("kv_append", q, d_v, n, H, dv, dt)
+        d.d_q, d.q_stride = self._heads_view("kv_append", q, d_q, n, QH, dk, dt)
+        d.d_q_out, d.q_out_stride = self._heads_view("kv_append", q, d_q_out, n, QH, dk, dt)
+        d.n_rows = self._table_rows("kv_append", q, d_table)
+        d.d_table, d.d_slot = d_table.data_ptr(), d_slot.data_ptr()
+        d.d_pos = d_pos.data_ptr() if d_pos is not None else None
+        if rope is not None:
+            d.rope = rope.desc
+        return self.lib.kv_append(self._h, C.byref(d), _stream_ptr(stream if stream is not None else self.compute))
+
+    def kv_attend_scratch_bytes(self, q, n_seqs, n_groups=0, max_suffix=0, max_prefix=0, max_members=0, weights=False):
+        return int(self.lib.kv_attend_scratch_bytes(self._h, int(q), int(n_seqs), int(n_groups), int(max_suffix),
+                                                    int(max_prefix), int(max_members), int(bool(weights))))
+
+    def kv_attend(self, q, layer, d_q, d_out, d_table, d_suffix, max_suffix, scale, d_scratch, d_prefix=None,
+                  d_group=None, max_prefix=0, max_members=0, d_lse=None, d_weight=None, stream=None):
+        """d_q, d_out: [sequences, query heads, dim]; d_suffix [sequences, 2], d_prefix [groups, 2] and d_group
+        [groups + 1] int32; d_lse float32 [sequences, query heads]; d_weight int64 [n_tags]."""
+        S, QH = d_q.shape[0], self.parts[q].n_q_heads
+        _, dk, dv = self._attention_dims(q)
+        dt = str(d_q.dtype)
+        if dt not in ("torch.bfloat16", "torch.float16"):
+            raise TypeError("kv_attend: queries of %s" % dt)
+        n_groups = d_prefix.shape[0] if d_prefix is not None else 0
+        _typed("kv_attend", [d_suffix, d_prefix, d_group], ("torch.int32", "torch.uint32"))
+        _typed("kv_attend", [d_lse], ("torch.float32",))
+        _typed("kv_attend", [d_weight], ("torch.int64", "torch.uint64"))
+        _plain("kv_attend", [d_suffix, d_prefix, d_group, d_lse, d_weight, d_scratch])
+        if (d_suffix.numel() != 2 * S or (d_prefix is not None and d_prefix.numel() != 2 * n_groups) or
+                (n_groups and (d_group is None or d_group.numel() != n_groups + 1)) or
+                (d_lse is not None and d_lse.numel() != S * QH) or (d_weight is not None and d_weight.numel() < self.n_tags)):
+            raise ValueError("kv_attend: arrays for %d sequences in %d groups have other sizes" % (S, n_groups))
+        d = kv_attend_desc(int(q), int(layer), KV_DTYPE_BF16 if dt == "torch.bfloat16" else KV_DTYPE_F16, float(scale),
+                           S, n_groups, int(max_suffix), int(max_prefix), int(max_members), 0)
+        d.d_q, d.q_stride = self._heads_view("kv_attend", q, d_q, S, QH, dk, dt)
+        d.d_out, d.out_stride = self._heads_view("kv_attend", q, d_out, S, QH, dv, dt)
+        d.n_rows = self._table_rows("kv_attend", q, d_table)
+        d.d_table, d.d_suffix = d_table.data_ptr(), d_suffix.data_ptr()
+        d.d_lse = d_lse.data_ptr() if d_lse is not None else None
+        d.d_prefix = d_prefix.data_ptr() if d_prefix is not None else None
+        d.d_group = d_group.data_ptr() if d_group is not None else None
+        d.d_weight = d_weight.data_ptr() if d_weight is not None else None
+        d.d_scratch, d.scratch_bytes = d_scratch.data_ptr(), d_scratch.numel() * d_scratch.element_size()
+        return self.lib.kv_attend(self._h, C.byref(d), _stream_ptr(stream if stream is not None else self.compute))
+
+    def kv_attention_score(self, epoch, decay, protect, d_weight, d_acc):
+        """d_weight int64 [n_tags] (cleared), d_acc float32 [n_tags]."""
+        _typed("kv_attention_score", [d_weight], ("torch.int64", "torch.uint64"))
+        _typed("kv_attention_score", [d_acc], ("torch.float32",))
+        _plain("kv_attention_score", [d_weight, d_acc])
+        if d_weight.numel() < self.n_tags or d_acc.numel() < self.n_tags:
+            raise ValueError("kv_attention_score: arrays of fewer than %d handles" % self.n_tags)
+        return self.lib.kv_attention_score(self._h, int(epoch), float(decay), int(protect), d_weight.data_ptr(),
+                                           d_acc.data_ptr(), _stream_ptr(self.compute))
 
     def kv_set_l2_residency(self, budget_bytes):
         return self.lib.kv_set_l2_residency(self._h, int(budget_bytes))

@@ -1,0 +1,859 @@
+// Attention of one query token per sequence over the pool's blocks; sequences of a group share a prefix
+// (kv_attend).
+//
+//   out_j = sum_t p_t v_t,  p_t = exp(scale q_j k_t - lse_j),  lse_j = log sum_t exp(scale q_j k_t)
+//
+// over the tokens t of the sequence's prefix and suffix whose blocks are in HBM.  The query heads of a
+// KV head -- of all members of a group, where it is a prefix -- are the rows of one small matrix product
+// per block, so that a block's K and V leave HBM once for all of them.  A segment's tokens are cut into
+// chunks that different CTAs work on; a part (one row, one chunk) is its normalised output and the log2 of
+// its sum of exponentials, and join_kernel adds the parts up with weights 2^(lse_part - lse).
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "kv_attend.cuh"
+
+namespace kvt {
+namespace {
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float exp2_(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float log2_(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// 16 bytes to shared memory, zeros if !there
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <typename T>
+__device__ __forceinline__ T narrow(float x);
+template <>
+__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <>
+__device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
+
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+  return fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __shfl_xor_sync(~0u, x, 1);
+  return x + __shfl_xor_sync(~0u, x, 2);
+}
+
+constexpr int kTile = 64;   // tokens of a tile
+
+// What a CTA works on: rows [row0, row0 + rows) of a segment and KV head, tokens [from, to) of it.
+struct Item {
+  Segment seg;
+  uint32_t index, head, row0, rows, seq0, from, to, chunk;
+  int kind;
+};
+
+// Item number i of the launch: kind's segments x heads x chunks x row tiles, row tiles innermost (they
+// read the same blocks).
+__device__ __forceinline__ bool item_of(const AttendArgs& a, int kind, uint32_t i, uint32_t row_tile, Item& w, bool tell) {
+  const uint32_t most = kind == kKindPrefix ? a.max_members * a.group : a.group;
+  const uint32_t tiles = (most + row_tile - 1u) / row_tile;
+  const uint32_t rt = i % tiles;
+  i /= tiles;
+  w.chunk = i % a.chunks[kind];
+  i /= a.chunks[kind];
+  w.head = i % a.tv.heads;
+  w.index = i / a.tv.heads;
+  w.kind = kind;
+  if (kind == kKindPrefix) {
+    uint32_t lo, hi;
+    a.members(w.index, lo, hi, tell);
+    w.seq0 = lo;
+    w.rows = (hi - lo) * a.group;
+    w.seg = a.checked(a.prefix, w.index, a.max_prefix, tell);
+  } else {
+    w.seq0 = w.index;
+    w.rows = a.group;
+    w.seg = a.checked(a.suffix, w.index, a.max_suffix, tell);
+  }
+  w.row0 = rt * row_tile;
+  w.from = w.chunk * a.chunk_tokens[kind];
+  if (w.row0 >= w.rows || (w.from >= w.seg.tokens && !(a.direct && w.chunk == 0))) return false;
+  w.rows = min(w.rows - w.row0, row_tile);
+  w.to = min(w.seg.tokens, w.from + a.chunk_tokens[kind]);
+  return true;
+}
+
+// Row r of an item: its sequence and query head.
+__device__ __forceinline__ void row_of(const AttendArgs& a, const Item& w, uint32_t r, uint32_t& seq, uint32_t& head) {
+  const uint32_t at = w.row0 + r, member = at / a.group;
+  seq = w.seq0 + member;
+  head = w.head * a.group + (at - member * a.group);
+}
+
+// Writes elements [d0, d0 + 2) of a row's part.
+template <typename T>
+__device__ __forceinline__ void put2(const AttendArgs& a, uint32_t seq, uint32_t head, uint32_t part, uint32_t d, float x, float y) {
+  if (a.direct) {
+    T* o = static_cast<T*>(a.out) + (int64_t)seq * a.out_seq + (int64_t)head * a.out_head + d;
+    o[0] = narrow<T>(x);
+    o[1] = narrow<T>(y);
+  } else {
+    float* o = a.part_o + (((uint64_t)seq * a.q_heads + head) * a.n_parts + part) * a.dv + d;
+    *reinterpret_cast<float2*>(o) = make_float2(x, y);
+  }
+}
+__device__ __forceinline__ void put_lse(const AttendArgs& a, uint32_t seq, uint32_t head, uint32_t part, float lse2) {
+  const uint64_t row = (uint64_t)seq * a.q_heads + head;
+  if (!a.direct || a.weight) a.part_lse[row * a.n_parts + part] = lse2;
+  if (a.direct && a.lse) a.lse[row] = lse2 * 0.69314718055994530942f;
+}
+
+__device__ __forceinline__ uint32_t part_of(const AttendArgs& a, const Item& w) {
+  return w.kind == kKindPrefix ? w.chunk : a.chunks[kKindPrefix] + w.chunk;
+}
+
+// A sequence without tokens, where no join follows.
+template <typename T>
+__device__ void put_nothing(const AttendArgs& a, const Item& w) {
+  for (uint32_t i = threadIdx.x; i < w.rows * (a.dv / 2u); i += blockDim.x) {
+    const uint32_t r = i / (a.dv / 2u), d = i % (a.dv / 2u) * 2u;
+    uint32_t seq, head;
+    row_of(a, w, r, seq, head);
+    put2<T>(a, seq, head, 0, d, 0.0f, 0.0f);
+    if (d == 0) put_lse(a, seq, head, 0, -INFINITY);
+  }
+}
+
+// Where the weight of grain `gr` of the item's segment for its first row goes.
+__device__ __forceinline__ float* grain_at(const AttendArgs& a, const Item& w, uint32_t gr) {
+  const uint64_t rows = w.kind == kKindPrefix ? (uint64_t)a.max_members * a.group : a.group;
+  return a.grain[w.kind] + (((uint64_t)w.index * a.tv.heads + w.head) * a.grains[w.kind] + gr) * rows + w.row0;
+}
+
+// Rows of up to 256 elements.  kM x kN warps: kM share out the rows (16 each), kN the tokens of a tile
+// (each then has its own maximum, sum and output, joined at the end).  K and V tiles of 64 tokens go through
+// shared memory in kStages stages filled by cp.async, 16-byte chunks of a row exchanged by row & 7, which
+// keeps ldmatrix free of bank conflicts.  Tokens that are not there are zeros in both tiles and -inf in the
+// scores, so nothing of what lies in such places reaches a sum.
+// Few rows (a suffix) are bound by HBM: the matrix instructions then run mostly empty, at about a fifth of
+// their rate.
+template <typename T, int D, int kM, int kN, int kStages>
+__global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constant__ AttendArgs a, uint32_t first_kind_items) {
+  constexpr int kWarps = kM * kN, kThreadsHere = kWarps * 32;
+  constexpr int kTok = kTile / kN;          // tokens of a warp in a tile
+  constexpr int kRowBytes = D * 2;
+  constexpr int kTileBytes = kTile * kRowBytes;
+  constexpr bool kQRegs = D <= 128;
+  extern __shared__ __align__(128) uint8_t smem[];
+  uint8_t* const kv = smem;                                    // [stages][K, V][64][D]
+  uint8_t* const q_s = smem + kStages * 2 * kTileBytes;        // [16 kM][D]
+  uint32_t* const chunk_s = reinterpret_cast<uint32_t*>(q_s + kM * 16 * kRowBytes);   // chunk of each block
+  wait_for_kernel_ahead();
+
+  Item w;
+  const bool second = blockIdx.x >= first_kind_items;
+  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? blockIdx.x - first_kind_items : blockIdx.x, kM * 16, w,
+               threadIdx.x == 0))
+    return;
+  if (w.to == 0) {
+    put_nothing<T>(a, w);
+    return;
+  }
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int wm = warp / kN, wn = warp % kN;
+  const TableView& tv = a.tv;
+  const uint32_t block0 = tv.by_tokens(w.from), blocks = tv.by_tokens(w.to - 1u) + 1u - block0;
+  for (uint32_t b = threadIdx.x; b < blocks; b += kThreadsHere) chunk_s[b] = tv.chunk((uint64_t)w.seg.row + block0 + b, w.head);
+
+  // queries: rows that are not there and dimensions beyond the head's are zeros
+  for (uint32_t i = threadIdx.x; i < kM * 16 * (D / 8); i += kThreadsHere) {
+    const uint32_t r = i / (D / 8), c = i % (D / 8);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < w.rows && c * 8u < a.dk) {
+      uint32_t seq, head;
+      row_of(a, w, r, seq, head);
+      const T* src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 8u;
+      if ((reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
+        v = *reinterpret_cast<const uint4*>(src);
+      } else {
+        uint16_t e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = reinterpret_cast<const uint16_t*>(src)[k];
+        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+      }
+    }
+    *reinterpret_cast<uint4*>(q_s + r * kRowBytes + ((c ^ (r & 7u)) * 16u)) = v;
+  }
+  __syncthreads();
+
+  const uint32_t tiles = (w.to - w.from + kTile - 1u) / kTile;
+  // tile `t` into stage t % kStages
+  auto fetch = [&](uint32_t t) {
+    uint8_t* const k_dst = kv + (t % kStages) * 2 * kTileBytes;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < kTile * (D / 8); i += kThreadsHere) {
+      const uint32_t tok = i / (D / 8), c = i % (D / 8);
+      const uint32_t at = w.from + t * kTile + tok, b = tv.by_tokens(at);
+      const uint32_t ch = at < w.to ? chunk_s[b - block0] : ~0u;
+      const bool there = ch != ~0u && c * 8u < a.dk;
+      const uint8_t* src = tv.slab;
+      if (there) src += (uint64_t)ch * tv.chunk_bytes + ((at - b * tv.block_tokens) * a.dk + c * 8u) * 2u;
+      const uint32_t off = tok * kRowBytes + ((c ^ (tok & 7u)) * 16u);
+      copy16(smem_u32(k_dst + off), src, there);
+      copy16(smem_u32(k_dst + kTileBytes + off), there ? src + (uint64_t)tv.heads * tv.chunk_bytes : src, there);
+    }
+  };
+#pragma unroll
+  for (int t = 0; t < kStages - 1; ++t) {
+    if ((uint32_t)t < tiles) fetch(t);
+    copy_commit();
+  }
+  const uint32_t q_row = wm * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
+  const uint32_t q_base = smem_u32(q_s + q_row * kRowBytes);
+  uint32_t qf[kQRegs ? D / 16 : 1][4];
+  if (kQRegs) {
+#pragma unroll
+    for (int k = 0; k < (kQRegs ? D / 16 : 1); ++k) ldmatrix4(qf[k], q_base + (((2 * k + (lane >> 4)) ^ (q_row & 7)) * 16));
+  }
+  float o[D / 8][4];
+#pragma unroll
+  for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+
+  for (uint32_t t = 0; t < tiles; ++t) {
+    copy_wait<kStages - 2>();
+    __syncthreads();   // tile t is there for every warp, and every warp is done with tile t - 1
+    if (t + kStages - 1 < tiles) fetch(t + kStages - 1);
+    copy_commit();
+    const uint8_t* const kt = kv + (t % kStages) * 2 * kTileBytes;
+    const uint8_t* const vt = kt + kTileBytes;
+    // scores of the warp's tokens
+    float s[kTok / 8][4];
+#pragma unroll
+    for (int j = 0; j < kTok / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      uint32_t qk[4];
+      if (kQRegs) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) qk[e] = qf[kQRegs ? k : 0][e];
+      } else {
+        ldmatrix4(qk, q_base + (((2 * k + (lane >> 4)) ^ (q_row & 7)) * 16));
+      }
+#pragma unroll
+      for (int j = 0; j < kTok / 16; ++j) {
+        const uint32_t tok = wn * kTok + j * 16 + (lane >> 4) * 8 + (lane & 7);
+        uint32_t b[4];
+        ldmatrix4(b, smem_u32(kt + tok * kRowBytes) + (((2 * k + (lane >> 3 & 1)) ^ (tok & 7)) * 16));
+        mma<T>(s[2 * j], qk, b[0], b[1]);
+        mma<T>(s[2 * j + 1], qk, b[2], b[3]);
+      }
+    }
+    // tokens that are not there
+    const uint32_t tok0 = w.from + t * kTile + wn * kTok;
+    bool all = tok0 + kTok <= w.to;
+    if (all) {
+      const uint32_t b1 = tv.by_tokens(tok0 + kTok - 1u) - block0;
+      for (uint32_t b = tv.by_tokens(tok0) - block0; b <= b1; ++b) all = all && chunk_s[b] != ~0u;
+    }
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < kTok / 8; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][e] *= a.scale2;
+      if (!all) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t at = tok0 + j * 8 + (lane & 3) * 2 + e;
+          if (at >= w.to || chunk_s[tv.by_tokens(at) - block0] == ~0u) s[j][e] = s[j][e + 2] = -INFINITY;
+        }
+      }
+      top[0] = fmaxf(top[0], fmaxf(s[j][0], s[j][1]));
+      top[1] = fmaxf(top[1], fmaxf(s[j][2], s[j][3]));
+    }
+    float base[2], turn[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float mx = fmaxf(m[r], quad_max(top[r]));
+      base[r] = mx == -INFINITY ? 0.0f : mx;     // nothing there so far
+      turn[r] = exp2_(m[r] - base[r]);
+      m[r] = mx;
+      l[r] *= turn[r];
+    }
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) {
+      o[j][0] *= turn[0];
+      o[j][1] *= turn[0];
+      o[j][2] *= turn[1];
+      o[j][3] *= turn[1];
+    }
+    if (a.weight && a.grain_tokens == 1u) {
+#pragma unroll
+      for (int j = 0; j < kTok / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t at = tok0 + j * 8 + (lane & 3) * 2 + (e & 1), r = wm * 16 + lane / 4 + (e >> 1) * 8;
+          if (at < w.to && r < w.rows) grain_at(a, w, at)[r] = s[j][e];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kTok / 16; ++j) {
+      float part[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int i = 2 * j; i < 2 * j + 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i][e] = exp2_(s[i][e] - base[e >> 1]);
+        part[0] += s[i][0] + s[i][1];
+        part[1] += s[i][2] + s[i][3];
+      }
+      l[0] += part[0];
+      l[1] += part[1];
+      if (a.weight && a.grain_tokens == 16u && tok0 + j * 16 < w.to) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float sum = quad_sum(part[h]);
+          const uint32_t r = wm * 16 + lane / 4 + h * 8;
+          if ((lane & 3) == 0 && r < w.rows) grain_at(a, w, (tok0 + j * 16) / 16u)[r] = base[h] + log2_(sum);
+        }
+      }
+      const uint32_t p[4] = {pack2<T>(s[2 * j][0], s[2 * j][1]), pack2<T>(s[2 * j][2], s[2 * j][3]),
+                             pack2<T>(s[2 * j + 1][0], s[2 * j + 1][1]), pack2<T>(s[2 * j + 1][2], s[2 * j + 1][3])};
+      const uint32_t tok = wn * kTok + j * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
+      const uint32_t v_base = smem_u32(vt + tok * kRowBytes);
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        uint32_t b[4];
+        ldmatrix4t(b, v_base + (((2 * d + (lane >> 4)) ^ (tok & 7)) * 16));
+        mma<T>(o[2 * d], p, b[0], b[1]);
+        mma<T>(o[2 * d + 1], p, b[2], b[3]);
+      }
+    }
+  }
+  l[0] = quad_sum(l[0]);
+  l[1] = quad_sum(l[1]);
+  const uint32_t part = part_of(a, w);
+  if (kN == 1) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t r = wm * 16 + lane / 4 + h * 8;
+      if (r >= w.rows) continue;
+      uint32_t seq, head;
+      row_of(a, w, r, seq, head);
+      const float inv = l[h] != 0.0f ? 1.0f / l[h] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) {
+        const uint32_t d = j * 8 + (lane & 3) * 2;
+        if (d < a.dv) put2<T>(a, seq, head, part, d, o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
+      }
+      if ((lane & 3) == 0) put_lse(a, seq, head, part, l[h] != 0.0f ? m[h] + log2_(l[h]) : -INFINITY);
+    }
+    return;
+  }
+  // the warps of a row join: maxima and sums, then outputs
+  copy_wait<0>();
+  __syncthreads();
+  float* const o_s = reinterpret_cast<float*>(smem);                          // [kN][16 kM][D]
+  float* const ml_s = o_s + kN * kM * 16 * D;                                 // [kN][16 kM][2]
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = wm * 16 + lane / 4 + h * 8;
+    if ((lane & 3) == 0) {
+      ml_s[(wn * kM * 16 + r) * 2] = m[h];
+      ml_s[(wn * kM * 16 + r) * 2 + 1] = l[h];
+    }
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j)
+      *reinterpret_cast<float2*>(o_s + (wn * kM * 16 + r) * D + ((j ^ (r & 7)) * 8 + (lane & 3) * 2)) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < kM * 16 * (D / 2); i += kThreadsHere) {
+    const uint32_t r = i / (D / 2), d = i % (D / 2) * 2u;
+    if (r >= w.rows || d >= a.dv) continue;
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) top = fmaxf(top, ml_s[(n * kM * 16 + r) * 2]);
+    const float from = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      const float c = exp2_(ml_s[(n * kM * 16 + r) * 2] - from);
+      const float2 v = *reinterpret_cast<const float2*>(o_s + (n * kM * 16 + r) * D + (((d / 8u) ^ (r & 7u)) * 8u + d % 8u));
+      sum += c * ml_s[(n * kM * 16 + r) * 2 + 1];
+      x += c * v.x;
+      y += c * v.y;
+    }
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    uint32_t seq, head;
+    row_of(a, w, r, seq, head);
+    put2<T>(a, seq, head, part, d, x * inv, y * inv);
+    if (d == 0) put_lse(a, seq, head, part, sum != 0.0f ? top + log2_(sum) : -INFINITY);
+  }
+}
+
+// MLA: one row per token is key (all dk elements) and value (the first dv) of every query head.  kM x kN warps:
+// kM share out the rows; for the scores kN share out the tokens of a tile, for the output its columns, so that a
+// warp's share of the 512 columns fits its registers.  Between the two the probabilities pass through shared memory.
+template <typename T, int kM, int kN>
+struct Latent {
+  static constexpr int D = 576, V = 512, kTok = kTile / kN, kCols = V / kN, kStages = 2;
+  static constexpr int kRowBytes = D * 2, kTileBytes = kTile * kRowBytes, kRows = kM * 16;
+  static constexpr size_t kSmem = kStages * kTileBytes + kRows * kRowBytes + kRows * kTile * 2 + 2 * kN * kRows * 4 + (kMaxChunkBlocks + 2) * 4;
+};
+
+template <typename T, int kM, int kN>
+__global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_constant__ AttendArgs a, uint32_t first_kind_items) {
+  using L = Latent<T, kM, kN>;
+  constexpr int kThreadsHere = kM * kN * 32, kRowBytes = L::kRowBytes, kRows = L::kRows, kTok = L::kTok, kCols = L::kCols;
+  extern __shared__ __align__(128) uint8_t smem[];
+  uint8_t* const kv = smem;
+  uint8_t* const q_s = kv + L::kStages * L::kTileBytes;                       // [rows][576]
+  uint8_t* const p_s = q_s + kRows * kRowBytes;                               // [rows][64]
+  float* const top_s = reinterpret_cast<float*>(p_s + kRows * kTile * 2);     // [kN][rows]
+  float* const sum_s = top_s + kN * kRows;                                    // [kN][rows]
+  uint32_t* const chunk_s = reinterpret_cast<uint32_t*>(sum_s + kN * kRows);
+  wait_for_kernel_ahead();
+  Item w;
+  const bool second = blockIdx.x >= first_kind_items;
+  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? blockIdx.x - first_kind_items : blockIdx.x, kRows, w, threadIdx.x == 0))
+    return;
+  if (w.to == 0) {
+    put_nothing<T>(a, w);
+    return;
+  }
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int wm = warp / kN, wn = warp % kN;
+  const TableView& tv = a.tv;
+  const uint32_t block0 = tv.by_tokens(w.from), blocks = tv.by_tokens(w.to - 1u) + 1u - block0;
+  for (uint32_t b = threadIdx.x; b < blocks; b += kThreadsHere) chunk_s[b] = tv.chunk((uint64_t)w.seg.row + block0 + b, w.head);
+  for (uint32_t i = threadIdx.x; i < kRows * (L::D / 8); i += kThreadsHere) {
+    const uint32_t r = i / (L::D / 8), c = i % (L::D / 8);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < w.rows && c * 8u < a.dk) {
+      uint32_t seq, head;
+      row_of(a, w, r, seq, head);
+      const T* src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 8u;
+      if ((reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
+        v = *reinterpret_cast<const uint4*>(src);
+      } else {
+        uint16_t e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = reinterpret_cast<const uint16_t*>(src)[k];
+        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
+      }
+    }
+    *reinterpret_cast<uint4*>(q_s + r * kRowBytes + ((c ^ (r & 7u)) * 16u)) = v;
+  }
+  __syncthreads();
+  const uint32_t tiles = (w.to - w.from + kTile - 1u) / kTile;
+  auto fetch = [&](uint32_t t) {
+    uint8_t* const dst = kv + (t % L::kStages) * L::kTileBytes;
+#pragma unroll 4
+    for (uint32_t i = threadIdx.x; i < kTile * (L::D / 8); i += kThreadsHere) {
+      const uint32_t tok = i / (L::D / 8), c = i % (L::D / 8);
+      const uint32_t at = w.from + t * kTile + tok, b = tv.by_tokens(at);
+      const uint32_t ch = at < w.to ? chunk_s[b - block0] : ~0u;
+      const bool there = ch != ~0u && c * 8u < a.dk;
+      const uint8_t* src = tv.slab;
+      if (there) src += (uint64_t)ch * tv.chunk_bytes + ((at - b * tv.block_tokens) * a.dk + c * 8u) * 2u;
+      copy16(smem_u32(dst + tok * kRowBytes + ((c ^ (tok & 7u)) * 16u)), src, there);
+    }
+  };
+  fetch(0);
+  copy_commit();
+  const uint32_t a_row = wm * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
+  const uint32_t q_base = smem_u32(q_s + a_row * kRowBytes), p_base = smem_u32(p_s + a_row * kTile * 2);
+  float o[kCols / 8][4];
+#pragma unroll
+  for (int j = 0; j < kCols / 8; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+
+  for (uint32_t t = 0; t < tiles; ++t) {
+    copy_wait<0>();
+    __syncthreads();
+    if (t + 1 < tiles) fetch(t + 1);
+    copy_commit();
+    const uint8_t* const kt = kv + (t % L::kStages) * L::kTileBytes;
+    float s[kTok / 8][4];
+#pragma unroll
+    for (int j = 0; j < kTok / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][e] = 0.0f;
+    const int steps = (a.dk + 15) / 16;
+#pragma unroll 4
+    for (int k = 0; k < steps; ++k) {
+      uint32_t qk[4];
+      ldmatrix4(qk, q_base + (((2 * k + (lane >> 4)) ^ (a_row & 7)) * 16));
+#pragma unroll
+      for (int j = 0; j < kTok / 16; ++j) {
+        const uint32_t tok = wn * kTok + j * 16 + (lane >> 4) * 8 + (lane & 7);
+        uint32_t b[4];
+        ldmatrix4(b, smem_u32(kt + tok * kRowBytes) + (((2 * k + (lane >> 3 & 1)) ^ (tok & 7)) * 16));
+        mma<T>(s[2 * j], qk, b[0], b[1]);
+        mma<T>(s[2 * j + 1], qk, b[2], b[3]);
+      }
+    }
+    const uint32_t tok0 = w.from + t * kTile + wn * kTok;
+    bool all = tok0 + kTok <= w.to;
+    if (all) {
+      const uint32_t b1 = tv.by_tokens(tok0 + kTok - 1u) - block0;
+      for (uint32_t b = tv.by_tokens(tok0) - block0; b <= b1; ++b) all = all && chunk_s[b] != ~0u;
+    }
+    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int j = 0; j < kTok / 8; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[j][e] *= a.scale2;
+      if (!all) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t at = tok0 + j * 8 + (lane & 3) * 2 + e;
+          if (at >= w.to || chunk_s[tv.by_tokens(at) - block0] == ~0u) s[j][e] = s[j][e + 2] = -INFINITY;
+        }
+      }
+      top[0] = fmaxf(top[0], fmaxf(s[j][0], s[j][1]));
+      top[1] = fmaxf(top[1], fmaxf(s[j][2], s[j][3]));
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      top[h] = quad_max(top[h]);
+      if ((lane & 3) == 0) top_s[wn * kRows + wm * 16 + lane / 4 + h * 8] = top[h];
+    }
+    __syncthreads();
+    float base[2], turn[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float mx = m[h];
+#pragma unroll
+      for (int n = 0; n < kN; ++n) mx = fmaxf(mx, top_s[n * kRows + wm * 16 + lane / 4 + h * 8]);
+      base[h] = mx == -INFINITY ? 0.0f : mx;
+      turn[h] = exp2_(m[h] - base[h]);
+      m[h] = mx;
+      l[h] *= turn[h];
+    }
+    if (a.weight && a.grain_tokens == 1u) {
+#pragma unroll
+      for (int j = 0; j < kTok / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t at = tok0 + j * 8 + (lane & 3) * 2 + (e & 1), r = wm * 16 + lane / 4 + (e >> 1) * 8;
+          if (at < w.to && r < w.rows) grain_at(a, w, at)[r] = s[j][e];
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kTok / 16; ++j) {
+      float part[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int i = 2 * j; i < 2 * j + 2; ++i) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i][e] = exp2_(s[i][e] - base[e >> 1]);
+        part[0] += s[i][0] + s[i][1];
+        part[1] += s[i][2] + s[i][3];
+        // 16-byte chunks of a row's 128 bytes are exchanged by row & 7, as in the tiles
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t r = wm * 16 + lane / 4 + h * 8, c = (wn * kTok + i * 8) / 8;
+          *reinterpret_cast<uint32_t*>(p_s + r * kTile * 2 + ((c ^ (r & 7u)) * 16u) + (lane & 3) * 4) = pack2<T>(s[i][2 * h], s[i][2 * h + 1]);
+        }
+      }
+      l[0] += part[0];
+      l[1] += part[1];
+      if (a.weight && a.grain_tokens == 16u && tok0 + j * 16 < w.to) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float sum = quad_sum(part[h]);
+          const uint32_t r = wm * 16 + lane / 4 + h * 8;
+          if ((lane & 3) == 0 && r < w.rows) grain_at(a, w, (tok0 + j * 16) / 16u)[r] = base[h] + log2_(sum);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kCols / 8; ++j) {
+      o[j][0] *= turn[0];
+      o[j][1] *= turn[0];
+      o[j][2] *= turn[1];
+      o[j][3] *= turn[1];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k) {
+      uint32_t p[4];
+      ldmatrix4(p, p_base + (((2 * k + (lane >> 4)) ^ (a_row & 7)) * 16));
+      const uint32_t tok = k * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
+      const uint32_t v_base = smem_u32(kt + tok * kRowBytes);
+#pragma unroll
+      for (int d = 0; d < kCols / 16; ++d) {
+        uint32_t b[4];
+        ldmatrix4t(b, v_base + (((wn * (kCols / 8) + 2 * d + (lane >> 4)) ^ (tok & 7)) * 16));
+        mma<T>(o[2 * d], p, b[0], b[1]);
+        mma<T>(o[2 * d + 1], p, b[2], b[3]);
+      }
+    }
+  }
+  // the sums of the kN warps' tokens
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    l[h] = quad_sum(l[h]);
+    if ((lane & 3) == 0) sum_s[wn * kRows + wm * 16 + lane / 4 + h * 8] = l[h];
+  }
+  __syncthreads();
+  const uint32_t part = part_of(a, w);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t r = wm * 16 + lane / 4 + h * 8;
+    if (r >= w.rows) continue;
+    float sum = 0.0f;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) sum += sum_s[n * kRows + r];
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    uint32_t seq, head;
+    row_of(a, w, r, seq, head);
+#pragma unroll
+    for (int j = 0; j < kCols / 8; ++j) {
+      const uint32_t d = wn * kCols + j * 8 + (lane & 3) * 2;
+      if (d < a.dv) put2<T>(a, seq, head, part, d, o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
+    }
+    if (wn == 0 && (lane & 3) == 0) put_lse(a, seq, head, part, sum != 0.0f ? m[h] + log2_(sum) : -INFINITY);
+  }
+}
+
+// ---- parts to outputs: a warp per (sequence, query head) -----------------------------------------
+
+constexpr int kJoinThreads = 128;
+
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a) {
+  wait_for_kernel_ahead();
+  const uint64_t row = (uint64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32;
+  const uint32_t lane = threadIdx.x % 32;
+  if (row >= (uint64_t)a.n_seqs * a.q_heads) return;
+  const uint32_t seq = (uint32_t)(row / a.q_heads), head = (uint32_t)(row - (uint64_t)seq * a.q_heads);
+  uint32_t np = 0;
+  if (a.n_groups) {
+    const uint32_t g = a.group_of(seq);
+    if (g != ~0u) {
+      const Segment p = a.checked(a.prefix, g, a.max_prefix, false);
+      np = (p.tokens + a.chunk_tokens[0] - 1u) / a.chunk_tokens[0];
+    }
+  }
+  const Segment sfx = a.checked(a.suffix, seq, a.max_suffix, false);
+  const uint32_t ns = (sfx.tokens + a.chunk_tokens[1] - 1u) / a.chunk_tokens[1];
+  const float* const lse = a.part_lse + row * a.n_parts;
+  auto place = [&](uint32_t i) { return i < np ? i : a.chunks[0] + i - np; };
+  float top = -INFINITY;
+  for (uint32_t i = lane; i < np + ns; i += 32) top = fmaxf(top, lse[place(i)]);
+#pragma unroll
+  for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
+  const float base = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+  for (uint32_t i = lane; i < np + ns; i += 32) sum += exp2_(lse[place(i)] - base);
+#pragma unroll
+  for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
+  const float total = sum != 0.0f ? base + log2_(sum) : -INFINITY;
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+  // (each lane's elements: two neighbours every 64)
+  for (uint32_t d0 = lane * 2u; d0 < a.dv; d0 += 64u) {
+    float x = 0.0f, y = 0.0f;
+    for (uint32_t i = 0; i < np + ns; ++i) {
+      const float e = lse[place(i)];
+      if (e == -INFINITY) continue;
+      const float c = exp2_(e - base) * inv;
+      const float2 v = *reinterpret_cast<const float2*>(a.part_o + (row * a.n_parts + place(i)) * a.dv + d0);
+      x = __fmaf_rn(c, v.x, x);
+      y = __fmaf_rn(c, v.y, y);
+    }
+    T* o = static_cast<T*>(a.out) + (int64_t)seq * a.out_seq + (int64_t)head * a.out_head + d0;
+    o[0] = narrow<T>(x);
+    o[1] = narrow<T>(y);
+  }
+  if (lane == 0) {
+    if (a.lse) a.lse[row] = total * 0.69314718055994530942f;
+    if (a.weight) a.part_lse[(uint64_t)a.n_seqs * a.q_heads * a.n_parts + row] = total;   // (what the weights are taken from)
+  }
+}
+
+// ---- grains to weights: a group of lanes per (segment, KV head, block) ------------------------------
+
+constexpr int kWeightThreads = 256;
+
+__global__ void __launch_bounds__(kWeightThreads) weight_kernel(const __grid_constant__ AttendArgs a, int kind, uint32_t blocks_most,
+                                                               uint32_t lanes) {
+  wait_for_kernel_ahead();
+  const uint64_t item = ((uint64_t)blockIdx.x * kWeightThreads + threadIdx.x) / lanes;
+  const uint32_t lane = threadIdx.x % lanes;
+  const uint32_t b = (uint32_t)(item % blocks_most);
+  const uint64_t sh = item / blocks_most;
+  const uint32_t head = (uint32_t)(sh % a.tv.heads);
+  const uint64_t index = sh / a.tv.heads;
+  unsigned long long w = 0;
+  uint32_t handle = KV_NONE;
+  if (index < (kind == kKindPrefix ? a.n_groups : a.n_seqs)) {
+    Segment seg;
+    uint32_t seq0 = (uint32_t)index, rows = a.group, stride = a.group;
+    if (kind == kKindPrefix) {
+      uint32_t lo, hi;
+      a.members((uint32_t)index, lo, hi, false);
+      seq0 = lo;
+      rows = (hi - lo) * a.group;
+      stride = a.max_members * a.group;
+      seg = a.checked(a.prefix, (uint32_t)index, a.max_prefix, false);
+    } else {
+      seg = a.checked(a.suffix, (uint32_t)index, a.max_suffix, false);
+    }
+    const uint32_t from = b * a.tv.block_tokens;
+    if (from < seg.tokens && rows) {
+      const uint64_t at = (uint64_t)seg.row + b;
+      if (a.tv.chunk(at, head) != ~0u) {
+        handle = a.tv.table[(at * a.tv.layers + a.tv.layer) * a.tv.heads + head];
+        const uint32_t to = min(seg.tokens, from + a.tv.block_tokens);
+        const uint32_t g0 = from / a.grain_tokens, g1 = (to + a.grain_tokens - 1u) / a.grain_tokens;
+        const float* const total = a.part_lse + (a.direct ? 0ull : (uint64_t)a.n_seqs * a.q_heads * a.n_parts);
+        const float* const grain = a.grain[kind] + (index * a.tv.heads + head) * (uint64_t)a.grains[kind] * stride;
+        float sum = 0.0f;
+        for (uint32_t r = lane; r < rows; r += lanes) {
+          const uint32_t member = r / a.group;
+          const float lse = total[(uint64_t)(seq0 + member) * a.q_heads + head * a.group + (r - member * a.group)];
+          if (lse == -INFINITY) continue;
+          for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r] - lse);
+        }
+        // in units of 2^-32; NaN counts as nothing
+        const float x = sum * 0x1p32f;
+        w = x > 0.0f ? __float2ull_rn(fminf(x, 0x1p62f)) : 0ull;
+      }
+    }
+  }
+  for (uint32_t d = lanes / 2u; d; d /= 2u) w += __shfl_xor_sync(~0u, w, d);
+  if (lane == 0 && w) atomicAdd(a.weight + handle, w);
+}
+
+// ---- launches ---------------------------------------------------------------------------------------
+
+template <typename F>
+cudaError_t launch_items(F* kernel, unsigned threads, size_t smem, const AttendArgs& a, uint32_t row_tile_prefix,
+                         uint32_t row_tile_suffix, bool prefix, bool suffix, cudaStream_t s) {
+  const uint64_t rows = (uint64_t)a.max_members * a.group;
+  const uint64_t np = prefix ? (rows + row_tile_prefix - 1) / row_tile_prefix * a.chunks[0] * a.tv.heads * a.n_groups : 0;
+  const uint64_t ns = suffix ? (a.group + row_tile_suffix - 1) / row_tile_suffix * (uint64_t)a.chunks[1] * a.tv.heads * a.n_seqs : 0;
+  if (np + ns == 0) return cudaSuccess;
+  if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  return launch_overlapped_smem(kernel, (unsigned)(np + ns), threads, smem, s, a, (uint32_t)np);
+}
+
+template <typename T, int D, int kM, int kN>
+cudaError_t launch_rows(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s) {
+  constexpr int kStages = D <= 64 ? 4 : (D <= 128 ? 3 : 2);
+  constexpr size_t tiles = (size_t)kStages * 2 * kTile * D * 2;
+  constexpr size_t join = kN > 1 ? (size_t)kN * kM * 16 * (D + 2) * 4 : 0;
+  static_assert(join <= tiles, "the join of the warps uses the tiles' memory");
+  return launch_items(rows_kernel<T, D, kM, kN, kStages>, kM * kN * 32, tiles + kM * 16 * D * 2 + (kMaxChunkBlocks + 2) * 4, a, kM * 16, kM * 16,
+                      prefix, suffix, s);
+}
+
+template <typename T, int D>
+cudaError_t launch_rows_by(const AttendArgs& a, uint32_t rows, bool prefix, bool suffix, cudaStream_t s) {
+  if (rows <= 16) return launch_rows<T, D, 1, 4>(a, prefix, suffix, s);
+  if (rows <= 32) return launch_rows<T, D, 2, 2>(a, prefix, suffix, s);
+  return launch_rows<T, D, 4, 1>(a, prefix, suffix, s);
+}
+
+template <typename T>
+cudaError_t launch_typed(const AttendArgs& a, bool mla, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  const bool prefix = a.chunks[0] > 0;
+  if (mla) {
+    using L = Latent<T, 4, 2>;
+    e = launch_items(latent_kernel<T, 4, 2>, 4 * 2 * 32, L::kSmem, a, L::kRows, L::kRows, prefix, true, s);
+  } else {
+    auto go = [&](uint32_t rows, bool p, bool f) {
+      return a.dk <= 64 ? launch_rows_by<T, 64>(a, rows, p, f, s) : a.dk <= 128 ? launch_rows_by<T, 128>(a, rows, p, f, s)
+                                                                               : launch_rows_by<T, 256>(a, rows, p, f, s);
+    };
+    const uint32_t rows = a.max_members * a.group;
+    auto size = [](uint32_t r) { return r <= 16 ? 1 : r <= 32 ? 2 : 4; };
+    if (prefix && size(rows) != size(a.group)) {
+      e = go(rows, true, false);
+      if (e == cudaSuccess) e = go(a.group, false, true);
+    } else {
+      e = go(a.group, prefix, true);
+    }
+  }
+  if (e != cudaSuccess) return e;
+  const uint64_t rows = (uint64_t)a.n_seqs * a.q_heads;
+  if (!a.direct)
+    e = launch_overlapped(join_kernel<T>, (unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)kJoinThreads, s, a);
+  if (e != cudaSuccess || !a.weight) return e;
+  for (int kind = prefix ? 0 : 1; kind < 2; ++kind) {
+    const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
+    const uint32_t blocks = (most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
+    if (!blocks) continue;
+    const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
+    uint32_t lanes = 1;
+    while (lanes < 32u && lanes < r) lanes *= 2u;
+    const uint64_t items = (uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks;
+    const uint64_t grid = (items * lanes + kWeightThreads - 1) / kWeightThreads;
+    if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
+    e = launch_overlapped(weight_kernel, (unsigned)grid, (unsigned)kWeightThreads, s, a, kind, blocks, lanes);
+    if (e != cudaSuccess) return e;
+  }
+  return e;
+}
+
+}  // namespace
+
+cudaError_t launch_attend(const AttendArgs& a, int dtype, bool mla, cudaStream_t s) {
+  return dtype == KV_DTYPE_BF16 ? launch_typed<__nv_bfloat16>(a, mla, s) : launch_typed<__half>(a, mla, s);
+}
+
+}  // namespace kvt

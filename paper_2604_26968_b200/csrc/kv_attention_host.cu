@@ -1,0 +1,252 @@
+// C ABI of the attention operators (kv_append, kv_attend, kv_attention_score): argument checks, the split of
+// the work, launches.
+#include <cmath>
+
+#include "kv_attend.cuh"
+
+using namespace kvt;
+
+namespace {
+
+inline cudaStream_t S(kv_stream_t s) { return static_cast<cudaStream_t>(s); }
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Elements of a query or key head and of a value head; a negative status if the operators do not take them.
+int32_t dims(const PoolView& v, int32_t q, uint32_t* dk, uint32_t* dv) {
+  const kv_model_desc& m = v.desc->part[q].model;
+  if (m.dtype_bits != 16 || m.n_q_heads <= 0) return KV_ERR_UNSUPPORTED_VARIANT;
+  const bool mla = v.variant[q] == KV_MLA;
+  *dk = (uint32_t)(mla ? m.d_latent + m.d_rope : m.head_dim);
+  *dv = (uint32_t)(mla ? m.d_latent : m.head_dim);
+  if (v.geom[q].heads > 4096u || (uint32_t)m.n_q_heads % v.geom[q].heads != 0) return KV_ERR_UNSUPPORTED_VARIANT;
+  return KV_OK;
+}
+
+TableView table_view(const PoolView& v, int32_t q, int32_t layer, const uint32_t* d_table, uint64_t n_rows) {
+  const PartGeom& g = v.geom[q];
+  TableView t;
+  t.table = d_table;
+  t.n_rows = n_rows;
+  t.loc = v.desc->d_loc;
+  t.n_tags = v.desc->n_tags < KV_NONE ? v.desc->n_tags : KV_NONE;
+  t.slab = g.slab;
+  t.base = g.base;
+  t.n = g.n;
+  t.heads = g.heads;
+  t.layers = (uint32_t)v.desc->part[q].model.n_layers;
+  t.layer = (uint32_t)layer;
+  t.n_chunks = g.n_chunks;
+  t.chunk_bytes = g.chunk_bytes;
+  t.block_tokens = (uint32_t)v.desc->part[q].block_tokens;
+  t.by_tokens = Divisor(t.block_tokens);
+  t.by_heads = Divisor(t.heads);
+  t.status = v.status;
+  return t;
+}
+
+// How a call's work is split: tokens of a chunk and chunks, for prefixes and suffixes.
+struct Split {
+  uint32_t chunk_tokens[2], chunks[2], n_parts, grain_tokens, grains[2];
+  uint64_t lse_at, grain_at[2], bytes;
+};
+
+// Chunks of a segment: enough CTAs for two full turns of the SMs (two resident on each), as long as a
+// chunk keeps 128 tokens.
+void split_segment(uint64_t ctas, uint32_t most, uint32_t block_tokens, uint32_t* chunk, uint32_t* chunks) {
+  const uint64_t target = 148u * 4u;
+  const uint64_t want = ctas ? (target + ctas - 1) / ctas : 1;
+  uint64_t c = ((uint64_t)most + want - 1) / want;
+  c = (c + 63) / 64 * 64;
+  if (c < 128) c = 128;
+  uint64_t limit = (uint64_t)kMaxChunkBlocks * block_tokens / 64 * 64;
+  if (limit < 64) limit = 64;
+  if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
+  if (c > limit) c = limit;
+  *chunk = (uint32_t)c;
+  *chunks = (uint32_t)(((uint64_t)most + c - 1) / c);
+}
+
+bool split(const PoolView& v, int32_t q, uint32_t dv, uint32_t n_seqs, uint32_t n_groups, uint32_t max_suffix,
+           uint32_t max_prefix, uint32_t max_members, bool weights, Split* out) {
+  const uint32_t bt = (uint32_t)v.desc->part[q].block_tokens, heads = v.geom[q].heads;
+  const uint32_t q_heads = (uint32_t)v.desc->part[q].model.n_q_heads, group = q_heads / heads;
+  const bool mla = v.variant[q] == KV_MLA;
+  const uint32_t tile = mla ? 64u : 16u;
+  const bool shared = n_groups && max_prefix && max_members;
+  // (per token of the longest run nothing may leave 31 bits)
+  if (max_suffix >= 0x40000000u || max_prefix >= 0x40000000u || n_seqs >= 0x1000000u || n_groups >= 0x1000000u) return false;
+  if (max_members > n_seqs) max_members = n_seqs;
+  if ((uint64_t)max_members * group >= 0x10000000u || (uint64_t)n_seqs * q_heads >= 0x40000000u) return false;
+  out->chunk_tokens[0] = out->chunk_tokens[1] = 64;
+  out->chunks[0] = out->chunks[1] = 0;
+  const uint64_t prefix_rows = (uint64_t)max_members * group;
+  const uint64_t row_tile = mla ? 64 : prefix_rows <= 16 ? 16 : prefix_rows <= 32 ? 32 : 64;
+  if (shared)
+    split_segment((prefix_rows + row_tile - 1) / row_tile * heads * n_groups, max_prefix, bt, &out->chunk_tokens[0], &out->chunks[0]);
+  split_segment((uint64_t)((group + tile - 1) / tile) * heads * n_seqs, max_suffix ? max_suffix : 1, bt, &out->chunk_tokens[1], &out->chunks[1]);
+  out->n_parts = out->chunks[0] + out->chunks[1];
+  out->grain_tokens = bt % 16 == 0 ? 16 : 1;
+  const unsigned __int128 rows = (unsigned __int128)n_seqs * q_heads;
+  unsigned __int128 at = 0;
+  auto take = [&at](unsigned __int128 bytes) { const uint64_t o = (uint64_t)at; at = (at + bytes + 255) / 256 * 256; return o; };
+  if (out->n_parts > 1) take(rows * out->n_parts * dv * 4);
+  out->lse_at = take(rows * (out->n_parts + 1) * 4);
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t most = k == 0 ? (shared ? max_prefix : 0) : max_suffix;
+    out->grains[k] = (uint32_t)(((uint64_t)most + out->grain_tokens - 1) / out->grain_tokens);
+    out->grain_at[k] = take(weights ? (unsigned __int128)(k == 0 ? n_groups : n_seqs) * heads * out->grains[k] *
+                                          (k == 0 ? prefix_rows : group) * 4
+                                    : 0);
+  }
+  if (at > ((unsigned __int128)1 << 46)) return false;
+  out->bytes = (uint64_t)at;
+  return true;
+}
+
+bool attend_dims(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv) {
+  if (v.variant[q] == KV_MLA) return dv <= 512 && dk <= kMaxRowDim && dk % 8 == 0 && dv % 8 == 0;
+  return dk <= 256 && dk % 8 == 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t kv_attend_scratch_bytes(kv_pool* p, int32_t q, uint32_t n_seqs, uint32_t n_groups, uint32_t max_suffix,
+                                 uint32_t max_prefix, uint32_t max_members, int32_t weights) {
+  if (!p) return 0;
+  const PoolView v = pool_view(p);
+  uint32_t dk, dv;
+  if (q < 0 || q >= v.n_parts || dims(v, q, &dk, &dv) != KV_OK || !attend_dims(v, q, dk, dv)) return 0;
+  Split s;
+  return split(v, q, dv, n_seqs, n_groups, max_suffix, max_prefix, max_members, weights != 0, &s) ? (s.bytes ? s.bytes : 256) : 0;
+}
+
+int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
+  if (!p || !d) return KV_ERR_INVALID_ARG;
+  const PoolView v = pool_view(p);
+  const int32_t q = d->partition;
+  if (q < 0 || q >= v.n_parts || d->layer < 0 || d->layer >= v.desc->part[q].model.n_layers) return KV_ERR_INVALID_ARG;
+  if (d->dtype != KV_DTYPE_BF16 && d->dtype != KV_DTYPE_F16) return KV_ERR_INVALID_ARG;
+  uint32_t dk, dv;
+  const int32_t rc = dims(v, q, &dk, &dv);
+  if (rc != KV_OK) return rc;
+  if (!attend_dims(v, q, dk, dv)) return KV_ERR_UNSUPPORTED_VARIANT;
+  if (!std::isfinite(d->scale)) return KV_ERR_INVALID_ARG;
+  if (d->n_seqs == 0) return KV_OK;
+  if (!d->d_q || !d->d_out || !aligned(d->d_q, 2) || !aligned(d->d_out, 2) || !d->d_suffix || !aligned(d->d_suffix, 4)) return KV_ERR_INVALID_ARG;
+  if (d->n_groups && (!d->d_prefix || !d->d_group || !aligned(d->d_prefix, 4) || !aligned(d->d_group, 4))) return KV_ERR_INVALID_ARG;
+  if (d->n_rows && (!d->d_table || !aligned(d->d_table, 4))) return KV_ERR_INVALID_ARG;
+  if (d->n_rows >= 0x100000000ull || !aligned(d->d_lse, 4) || !aligned(d->d_weight, 8)) return KV_ERR_INVALID_ARG;
+  Split sp;
+  if (!split(v, q, dv, d->n_seqs, d->n_groups, d->max_suffix, d->max_prefix, d->max_members, d->d_weight != nullptr, &sp)) return KV_ERR_INVALID_ARG;
+  if (!d->d_scratch || !aligned(d->d_scratch, 16) || d->scratch_bytes < sp.bytes) return KV_ERR_INVALID_ARG;
+  const int32_t rs = pool_settle(p, stream);
+  if (rs != KV_OK) return rs;
+  AttendArgs a{};
+  a.tv = table_view(v, q, d->layer, d->d_table, d->n_rows);
+  a.q = d->d_q;
+  a.out = d->d_out;
+  a.lse = d->d_lse;
+  a.q_seq = d->q_stride[0];
+  a.q_head = d->q_stride[1];
+  a.out_seq = d->out_stride[0];
+  a.out_head = d->out_stride[1];
+  a.scale2 = d->scale * 1.44269504088896340736f;
+  a.n_seqs = d->n_seqs;
+  a.n_groups = sp.chunks[0] ? d->n_groups : 0u;
+  a.q_heads = (uint32_t)v.desc->part[q].model.n_q_heads;
+  a.group = a.q_heads / a.tv.heads;
+  a.dk = dk;
+  a.dv = dv;
+  a.suffix = d->d_suffix;
+  a.prefix = d->d_prefix;
+  a.group_start = d->d_group;
+  a.max_suffix = d->max_suffix;
+  a.max_prefix = d->max_prefix;
+  a.max_members = d->max_members < d->n_seqs ? d->max_members : d->n_seqs;
+  uint8_t* const scratch = static_cast<uint8_t*>(d->d_scratch);
+  for (int k = 0; k < 2; ++k) {
+    a.chunk_tokens[k] = sp.chunk_tokens[k];
+    a.chunks[k] = sp.chunks[k];
+    a.grains[k] = sp.grains[k];
+    a.grain[k] = reinterpret_cast<float*>(scratch + sp.grain_at[k]);
+  }
+  a.n_parts = sp.n_parts;
+  a.direct = sp.n_parts == 1;
+  a.part_o = reinterpret_cast<float*>(scratch);
+  a.part_lse = reinterpret_cast<float*>(scratch + sp.lse_at);
+  a.grain_tokens = sp.grain_tokens;
+  a.weight = reinterpret_cast<unsigned long long*>(d->d_weight);
+  return pool_cuda_error(p, launch_attend(a, d->dtype, v.variant[q] == KV_MLA, S(stream)));
+}
+
+int32_t kv_append(kv_pool* p, const kv_append_desc* d, kv_stream_t stream) {
+  if (!p || !d) return KV_ERR_INVALID_ARG;
+  const PoolView v = pool_view(p);
+  const int32_t q = d->partition;
+  if (q < 0 || q >= v.n_parts || d->layer < 0 || d->layer >= v.desc->part[q].model.n_layers) return KV_ERR_INVALID_ARG;
+  if (d->dtype != KV_DTYPE_BF16 && d->dtype != KV_DTYPE_F16) return KV_ERR_INVALID_ARG;
+  uint32_t dk, dv;
+  const int32_t rc = dims(v, q, &dk, &dv);
+  if (rc != KV_OK) return rc;
+  const bool mla = v.variant[q] == KV_MLA;
+  const kv_rope_desc& r = d->rope;
+  if (r.rot_dim < 0 || r.rot_dim > 256 || r.rot_dim % 2 != 0 || r.rot_first < 0 ||
+      (int64_t)r.rot_first + r.rot_dim > (int64_t)dk)
+    return KV_ERR_INVALID_ARG;
+  if (r.rot_dim > 0) {
+    if (r.n_axes < 1 || r.n_axes > 4) return KV_ERR_INVALID_ARG;
+    for (int i = 0; i < r.rot_dim / 2; ++i)
+      if (r.axis[i] >= r.n_axes) return KV_ERR_INVALID_ARG;
+  }
+  if (d->n_tokens == 0) return KV_OK;
+  if (r.rot_dim > 0 && (!r.d_inv_freq || !aligned(r.d_inv_freq, 4) || !d->d_pos || !aligned(d->d_pos, 4))) return KV_ERR_INVALID_ARG;
+  if (d->n_tokens > 0x7fffffffull || d->n_rows >= 0x100000000ull) return KV_ERR_INVALID_ARG;
+  if (!d->d_k || !aligned(d->d_k, 2) || (mla ? d->d_v != nullptr : !d->d_v) || !aligned(d->d_v, 2)) return KV_ERR_INVALID_ARG;
+  if ((d->d_q != nullptr) != (d->d_q_out != nullptr) || !aligned(d->d_q, 2) || !aligned(d->d_q_out, 2)) return KV_ERR_INVALID_ARG;
+  if (!d->d_slot || !aligned(d->d_slot, 8) || (d->n_rows && (!d->d_table || !aligned(d->d_table, 4)))) return KV_ERR_INVALID_ARG;
+  const int32_t rs = pool_settle(p, stream);
+  if (rs != KV_OK) return rs;
+  AppendArgs a{};
+  a.tv = table_view(v, q, d->layer, d->d_table, d->n_rows);
+  a.k = d->d_k;
+  a.v = d->d_v;
+  a.q = d->d_q;
+  a.q_out = d->d_q_out;
+  a.k_tok = d->k_stride[0]; a.k_head = d->k_stride[1];
+  a.v_tok = d->v_stride[0]; a.v_head = d->v_stride[1];
+  a.q_tok = d->q_stride[0]; a.q_head = d->q_stride[1];
+  a.o_tok = d->q_out_stride[0]; a.o_head = d->q_out_stride[1];
+  a.slot = d->d_slot;
+  a.pos = d->d_pos;
+  a.inv_freq = r.d_inv_freq;
+  a.n = d->n_tokens;
+  a.q_heads = d->d_q ? (uint32_t)v.desc->part[q].model.n_q_heads : 0u;
+  a.dk = dk;
+  a.dv = mla ? 0u : dv;
+  a.rot_first = (uint32_t)r.rot_first;
+  a.rot_dim = (uint32_t)r.rot_dim;
+  a.interleaved = r.interleaved != 0;
+  a.n_axes = (uint32_t)r.n_axes;
+  for (int i = 0; i < 128; ++i) a.axis[i] = r.axis[i];
+  // 16-byte vectors where every one of them is aligned; blocks always are, if their rows are
+  auto strides = [](const int64_t (&s)[2]) { return s[0] % 8 == 0 && s[1] % 8 == 0; };
+  const bool wide = dk % 8 == 0 && a.dv % 8 == 0 && a.rot_first % 8 == 0 && a.rot_dim % (a.interleaved ? 8 : 16) == 0 &&
+                    aligned(d->d_k, 16) && strides(d->k_stride) && (mla || (aligned(d->d_v, 16) && strides(d->v_stride))) &&
+                    (!d->d_q || (aligned(d->d_q, 16) && strides(d->q_stride) && aligned(d->d_q_out, 16) && strides(d->q_out_stride)));
+  return pool_cuda_error(p, launch_append(a, d->dtype, wide, S(stream)));
+}
+
+int32_t kv_attention_score(kv_pool* p, uint32_t epoch, float decay, uint32_t protect, uint64_t* d_weight, float* d_acc,
+                           kv_stream_t stream) {
+  if (!p || !(decay >= 0.0f && decay <= 1.0f) || protect >= 0x80000000u) return KV_ERR_INVALID_ARG;
+  if (!d_weight || !d_acc || !aligned(d_weight, 16) || !aligned(d_acc, 16)) return KV_ERR_INVALID_ARG;
+  const int32_t rs = pool_settle(p, stream);
+  if (rs != KV_OK) return rs;
+  const PoolView v = pool_view(p);
+  return pool_cuda_error(p, launch_attention_score(v.st, epoch, decay, protect, reinterpret_cast<unsigned long long*>(d_weight), d_acc,
+                                                   v.desc->n_tags, v.status, S(stream)));
+}
+
+}  // extern "C"

@@ -9,6 +9,7 @@
 #include <utility>
 #include <vector>
 
+#include "kv_attend.cuh"
 #include "kvtier_internal.cuh"
 
 using namespace kvt;
@@ -502,6 +503,23 @@ int32_t join_promotions(kv_pool* p, cudaStream_t s, int q_only = -1) {
   } while (0)
 
 }  // namespace
+
+namespace kvt {
+
+PoolView pool_view(kv_pool* p) {
+  PoolView v{&p->desc, p->geom, p->n_parts, p->st, p->ws.status, {}};
+  for (int q = 0; q < p->n_parts; ++q) v.variant[q] = p->host[q].variant;
+  return v;
+}
+
+int32_t pool_settle(kv_pool* p, kv_stream_t stream) {
+  KV_SETTLE(p, stream);
+  return KV_OK;
+}
+
+int32_t pool_cuda_error(kv_pool* p, cudaError_t e) { return e == cudaSuccess ? KV_OK : cuda_fail(p, e); }
+
+}  // namespace kvt
 
 extern "C" {
 

@@ -8,25 +8,11 @@
 // per block, so that a block's K and V leave HBM once for all of them.  A segment's tokens are cut into
 // chunks that different CTAs work on; a part (one row, one chunk) is its normalised output and the log2 of
 // its sum of exponentials, and join_kernel adds the parts up with weights 2^(lse_part - lse).
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
-#include "kv_attend.cuh"
+#include "kv_attend_device.cuh"
 
 namespace kvt {
 namespace {
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ float exp2_(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ float log2_(float x) {
-  float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // 16 bytes to shared memory, zeros if !there
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -60,25 +46,6 @@ __device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <typename T>
-__device__ __forceinline__ uint32_t pack2(float lo, float hi);
-template <>
-__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-template <>
-__device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
-  const __half2 v = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-template <typename T>
-__device__ __forceinline__ T narrow(float x);
-template <>
-__device__ __forceinline__ __nv_bfloat16 narrow<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
-template <>
-__device__ __forceinline__ __half narrow<__half>(float x) { return __float2half_rn(x); }
-
 __device__ __forceinline__ float quad_max(float x) {
   x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
   return fmaxf(x, __shfl_xor_sync(~0u, x, 2));
@@ -89,91 +56,6 @@ __device__ __forceinline__ float quad_sum(float x) {
 }
 
 constexpr int kTile = 64;   // tokens of a tile
-
-// What a CTA works on: rows [row0, row0 + rows) of a segment and KV head, tokens [from, to) of it.
-struct Item {
-  Segment seg;
-  uint32_t index, head, row0, rows, seq0, from, to, chunk;
-  int kind;
-};
-
-// Item number i of the launch: kind's segments x heads x chunks x row tiles, row tiles innermost (they
-// read the same blocks).
-__device__ __forceinline__ bool item_of(const AttendArgs& a, int kind, uint32_t i, uint32_t row_tile, Item& w, bool tell) {
-  const uint32_t most = kind == kKindPrefix ? a.max_members * a.group : a.group;
-  const uint32_t tiles = (most + row_tile - 1u) / row_tile;
-  const uint32_t rt = i % tiles;
-  i /= tiles;
-  w.chunk = i % a.chunks[kind];
-  i /= a.chunks[kind];
-  w.head = i % a.tv.heads;
-  w.index = i / a.tv.heads;
-  w.kind = kind;
-  if (kind == kKindPrefix) {
-    uint32_t lo, hi;
-    a.members(w.index, lo, hi, tell);
-    w.seq0 = lo;
-    w.rows = (hi - lo) * a.group;
-    w.seg = a.checked(a.prefix, w.index, a.max_prefix, tell);
-  } else {
-    w.seq0 = w.index;
-    w.rows = a.group;
-    w.seg = a.checked(a.suffix, w.index, a.max_suffix, tell);
-  }
-  w.row0 = rt * row_tile;
-  w.from = w.chunk * a.chunk_tokens[kind];
-  if (w.row0 >= w.rows || (w.from >= w.seg.tokens && !(a.direct && w.chunk == 0))) return false;
-  w.rows = min(w.rows - w.row0, row_tile);
-  w.to = min(w.seg.tokens, w.from + a.chunk_tokens[kind]);
-  return true;
-}
-
-// Row r of an item: its sequence and query head.
-__device__ __forceinline__ void row_of(const AttendArgs& a, const Item& w, uint32_t r, uint32_t& seq, uint32_t& head) {
-  const uint32_t at = w.row0 + r, member = at / a.group;
-  seq = w.seq0 + member;
-  head = w.head * a.group + (at - member * a.group);
-}
-
-// Writes elements [d0, d0 + 2) of a row's part.
-template <typename T>
-__device__ __forceinline__ void put2(const AttendArgs& a, uint32_t seq, uint32_t head, uint32_t part, uint32_t d, float x, float y) {
-  if (a.direct) {
-    T* o = static_cast<T*>(a.out) + (int64_t)seq * a.out_seq + (int64_t)head * a.out_head + d;
-    o[0] = narrow<T>(x);
-    o[1] = narrow<T>(y);
-  } else {
-    float* o = a.part_o + (((uint64_t)seq * a.q_heads + head) * a.n_parts + part) * a.dv + d;
-    *reinterpret_cast<float2*>(o) = make_float2(x, y);
-  }
-}
-__device__ __forceinline__ void put_lse(const AttendArgs& a, uint32_t seq, uint32_t head, uint32_t part, float lse2) {
-  const uint64_t row = (uint64_t)seq * a.q_heads + head;
-  if (!a.direct || a.weight) a.part_lse[row * a.n_parts + part] = lse2;
-  if (a.direct && a.lse) a.lse[row] = lse2 * 0.69314718055994530942f;
-}
-
-__device__ __forceinline__ uint32_t part_of(const AttendArgs& a, const Item& w) {
-  return w.kind == kKindPrefix ? w.chunk : a.chunks[kKindPrefix] + w.chunk;
-}
-
-// A sequence without tokens, where no join follows.
-template <typename T>
-__device__ void put_nothing(const AttendArgs& a, const Item& w) {
-  for (uint32_t i = threadIdx.x; i < w.rows * (a.dv / 2u); i += blockDim.x) {
-    const uint32_t r = i / (a.dv / 2u), d = i % (a.dv / 2u) * 2u;
-    uint32_t seq, head;
-    row_of(a, w, r, seq, head);
-    put2<T>(a, seq, head, 0, d, 0.0f, 0.0f);
-    if (d == 0) put_lse(a, seq, head, 0, -INFINITY);
-  }
-}
-
-// Where the weight of grain `gr` of the item's segment for its first row goes.
-__device__ __forceinline__ float* grain_at(const AttendArgs& a, const Item& w, uint32_t gr) {
-  const uint64_t rows = w.kind == kKindPrefix ? (uint64_t)a.max_members * a.group : a.group;
-  return a.grain[w.kind] + (((uint64_t)w.index * a.tv.heads + w.head) * a.grains[w.kind] + gr) * rows + w.row0;
-}
 
 // Rows of up to 256 elements.  kM x kN warps: kM share out the rows (16 each), kN the tokens of a tile
 // (each then has its own maximum, sum and output, joined at the end).  K and V tiles of 64 tokens go through
@@ -217,15 +99,7 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
     if (r < w.rows && c * 8u < a.dk) {
       uint32_t seq, head;
       row_of(a, w, r, seq, head);
-      const T* src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 8u;
-      if ((reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
-        v = *reinterpret_cast<const uint4*>(src);
-      } else {
-        uint16_t e[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] = reinterpret_cast<const uint16_t*>(src)[k];
-        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
-      }
+      v = load8(static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 8u);
     }
     *reinterpret_cast<uint4*>(q_s + r * kRowBytes + ((c ^ (r & 7u)) * 16u)) = v;
   }
@@ -244,8 +118,8 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
       const uint8_t* src = tv.slab;
       if (there) src += (uint64_t)ch * tv.chunk_bytes + ((at - b * tv.block_tokens) * a.dk + c * 8u) * 2u;
       const uint32_t off = tok * kRowBytes + ((c ^ (tok & 7u)) * 16u);
-      copy16(smem_u32(k_dst + off), src, there);
-      copy16(smem_u32(k_dst + kTileBytes + off), there ? src + (uint64_t)tv.heads * tv.chunk_bytes : src, there);
+      copy16(smem_address(k_dst + off), src, there);
+      copy16(smem_address(k_dst + kTileBytes + off), there ? src + (uint64_t)tv.heads * tv.chunk_bytes : src, there);
     }
   };
 #pragma unroll
@@ -254,7 +128,7 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
     copy_commit();
   }
   const uint32_t q_row = wm * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
-  const uint32_t q_base = smem_u32(q_s + q_row * kRowBytes);
+  const uint32_t q_base = smem_address(q_s + q_row * kRowBytes);
   uint32_t qf[kQRegs ? D / 16 : 1][4];
   if (kQRegs) {
 #pragma unroll
@@ -293,7 +167,7 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
       for (int j = 0; j < kTok / 16; ++j) {
         const uint32_t tok = wn * kTok + j * 16 + (lane >> 4) * 8 + (lane & 7);
         uint32_t b[4];
-        ldmatrix4(b, smem_u32(kt + tok * kRowBytes) + (((2 * k + (lane >> 3 & 1)) ^ (tok & 7)) * 16));
+        ldmatrix4(b, smem_address(kt + tok * kRowBytes) + (((2 * k + (lane >> 3 & 1)) ^ (tok & 7)) * 16));
         mma<T>(s[2 * j], qk, b[0], b[1]);
         mma<T>(s[2 * j + 1], qk, b[2], b[3]);
       }
@@ -368,7 +242,7 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
       const uint32_t p[4] = {pack2<T>(s[2 * j][0], s[2 * j][1]), pack2<T>(s[2 * j][2], s[2 * j][3]),
                              pack2<T>(s[2 * j + 1][0], s[2 * j + 1][1]), pack2<T>(s[2 * j + 1][2], s[2 * j + 1][3])};
       const uint32_t tok = wn * kTok + j * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
-      const uint32_t v_base = smem_u32(vt + tok * kRowBytes);
+      const uint32_t v_base = smem_address(vt + tok * kRowBytes);
 #pragma unroll
       for (int d = 0; d < D / 16; ++d) {
         uint32_t b[4];
@@ -480,15 +354,7 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
     if (r < w.rows && c * 8u < a.dk) {
       uint32_t seq, head;
       row_of(a, w, r, seq, head);
-      const T* src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 8u;
-      if ((reinterpret_cast<uintptr_t>(src) & 15u) == 0) {
-        v = *reinterpret_cast<const uint4*>(src);
-      } else {
-        uint16_t e[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) e[k] = reinterpret_cast<const uint16_t*>(src)[k];
-        v = make_uint4(e[0] | (uint32_t)e[1] << 16, e[2] | (uint32_t)e[3] << 16, e[4] | (uint32_t)e[5] << 16, e[6] | (uint32_t)e[7] << 16);
-      }
+      v = load8(static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 8u);
     }
     *reinterpret_cast<uint4*>(q_s + r * kRowBytes + ((c ^ (r & 7u)) * 16u)) = v;
   }
@@ -504,13 +370,13 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
       const bool there = ch != ~0u && c * 8u < a.dk;
       const uint8_t* src = tv.slab;
       if (there) src += (uint64_t)ch * tv.chunk_bytes + ((at - b * tv.block_tokens) * a.dk + c * 8u) * 2u;
-      copy16(smem_u32(dst + tok * kRowBytes + ((c ^ (tok & 7u)) * 16u)), src, there);
+      copy16(smem_address(dst + tok * kRowBytes + ((c ^ (tok & 7u)) * 16u)), src, there);
     }
   };
   fetch(0);
   copy_commit();
   const uint32_t a_row = wm * 16 + (lane & 7) + (lane >> 3 & 1) * 8;
-  const uint32_t q_base = smem_u32(q_s + a_row * kRowBytes), p_base = smem_u32(p_s + a_row * kTile * 2);
+  const uint32_t q_base = smem_address(q_s + a_row * kRowBytes), p_base = smem_address(p_s + a_row * kTile * 2);
   float o[kCols / 8][4];
 #pragma unroll
   for (int j = 0; j < kCols / 8; ++j)
@@ -538,7 +404,7 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
       for (int j = 0; j < kTok / 16; ++j) {
         const uint32_t tok = wn * kTok + j * 16 + (lane >> 4) * 8 + (lane & 7);
         uint32_t b[4];
-        ldmatrix4(b, smem_u32(kt + tok * kRowBytes) + (((2 * k + (lane >> 3 & 1)) ^ (tok & 7)) * 16));
+        ldmatrix4(b, smem_address(kt + tok * kRowBytes) + (((2 * k + (lane >> 3 & 1)) ^ (tok & 7)) * 16));
         mma<T>(s[2 * j], qk, b[0], b[1]);
         mma<T>(s[2 * j + 1], qk, b[2], b[3]);
       }
@@ -630,7 +496,7 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
       uint32_t p[4];
       ldmatrix4(p, p_base + (((2 * k + (lane >> 4)) ^ (a_row & 7)) * 16));
       const uint32_t tok = k * 16 + (lane >> 3 & 1) * 8 + (lane & 7);
-      const uint32_t v_base = smem_u32(kt + tok * kRowBytes);
+      const uint32_t v_base = smem_address(kt + tok * kRowBytes);
 #pragma unroll
       for (int d = 0; d < kCols / 16; ++d) {
         uint32_t b[4];
@@ -809,24 +675,26 @@ cudaError_t launch_rows_by(const AttendArgs& a, uint32_t rows, bool prefix, bool
 }
 
 template <typename T>
-cudaError_t launch_typed(const AttendArgs& a, bool mla, cudaStream_t s) {
+cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  const bool prefix = a.chunks[0] > 0;
+  const bool prefix = a.chunks[0] > 0, tp = prefix && a.tiles[0], ts = a.tiles[1], rp = prefix && !tp, rs = !ts;
+  if (tp || ts) e = launch_attend_tiles(a, dtype, mla, tp, ts, s);
+  if (e != cudaSuccess) return e;
   if (mla) {
     using L = Latent<T, 4, 2>;
-    e = launch_items(latent_kernel<T, 4, 2>, 4 * 2 * 32, L::kSmem, a, L::kRows, L::kRows, prefix, true, s);
-  } else {
+    if (rp || rs) e = launch_items(latent_kernel<T, 4, 2>, 4 * 2 * 32, L::kSmem, a, L::kRows, L::kRows, rp, rs, s);
+  } else if (rp || rs) {
     auto go = [&](uint32_t rows, bool p, bool f) {
       return a.dk <= 64 ? launch_rows_by<T, 64>(a, rows, p, f, s) : a.dk <= 128 ? launch_rows_by<T, 128>(a, rows, p, f, s)
                                                                                : launch_rows_by<T, 256>(a, rows, p, f, s);
     };
     const uint32_t rows = a.max_members * a.group;
     auto size = [](uint32_t r) { return r <= 16 ? 1 : r <= 32 ? 2 : 4; };
-    if (prefix && size(rows) != size(a.group)) {
+    if (rp && (!rs || size(rows) != size(a.group))) {
       e = go(rows, true, false);
-      if (e == cudaSuccess) e = go(a.group, false, true);
+      if (e == cudaSuccess && rs) e = go(a.group, false, true);
     } else {
-      e = go(a.group, prefix, true);
+      e = go(a.group, rp, rs);
     }
   }
   if (e != cudaSuccess) return e;
@@ -853,7 +721,7 @@ cudaError_t launch_typed(const AttendArgs& a, bool mla, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_attend(const AttendArgs& a, int dtype, bool mla, cudaStream_t s) {
-  return dtype == KV_DTYPE_BF16 ? launch_typed<__nv_bfloat16>(a, mla, s) : launch_typed<__half>(a, mla, s);
+  return dtype == KV_DTYPE_BF16 ? launch_typed<__nv_bfloat16>(a, dtype, mla, s) : launch_typed<__half>(a, dtype, mla, s);
 }
 
 }  // namespace kvt

@@ -1,0 +1,611 @@
+// kv_attend where a block is read by many rows: tiles on the fifth-generation tensor cores.
+//
+// A row tile is 128 rows (query heads of the members of a group, or of a sequence): its scores
+// S = Q K^T and its output O = P V are accumulators in tensor memory, 128 lanes x a column for each token or
+// output element.  Blocks come by TMA, a box of one block x 64 elements (128 bytes, swizzled), so that a tile
+// of tokens lies in shared memory as the matrix instructions want it whatever blocks it is made of; a block
+// that is not there is a box outside the tensor, which reads as zeros.
+//
+// Roles: warp 0 looks blocks up and issues the copies, one thread of warp 1 issues the matrix
+// instructions, and each further group of four warps is a row tile's softmax, a thread per row: it reads its row
+// of S, keeps maximum and sum, and writes the probabilities over S, from where P V takes them as the operand
+// in tensor memory.  With two row tiles (kTiles == 2) the tensor cores work on one's products while the
+// other's probabilities are formed; with one (kTiles == 1, MLA) S has two places and the scores of
+// the next tokens are formed meanwhile.  The output is rescaled only when a row's maximum has grown by
+// more than 2^8 since the last time (its sum is kept to the same base, so that results are what they were).
+//
+// MLA: a row of 576 elements is key (all of them) and value (the first 512).  128 x 512 outputs would
+// fill the tensor memory, so a CTA takes 256 of the columns, and both CTAs form the scores.  The first 256 elements
+// of Q lie in tensor memory, which leaves room for two tiles of 64 tokens in shared memory.
+//
+// Every wait is bounded: one that gives up sets KV_DEV_WAIT_EXPIRED and a flag that ends the other
+// waits; copies and matrix instructions in flight are then waited for (bounded) before the CTA leaves.
+#include <cuda.h>
+
+#include "kv_attend_device.cuh"
+
+namespace kvt {
+namespace {
+
+constexpr unsigned long long kWaitLimit = 2'000'000'000ull;   // nanoseconds
+
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(done)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return done != 0;
+}
+// False: this wait, or another of the CTA, has given up.
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t* status) {
+  if (bar_try(bar, parity)) return true;
+  unsigned long long from, now;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(from));
+  do {
+    for (int i = 0; i < 64; ++i) {
+      if (bar_try(bar, parity)) return true;
+      if (*gave_up) return false;
+    }
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+  } while (now - from < kWaitLimit);
+  *gave_up = 1u;
+  atomicOr(status, KV_DEV_WAIT_EXPIRED);
+  return false;
+}
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// D (+)= A B, A and B from shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+// A from tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      : "memory");
+}
+#define KVT_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define KVT_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of the thread's lane
+__device__ __forceinline__ void tmem_load(uint32_t* r, uint32_t at) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+      "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : KVT_R8(r, 0), KVT_R8(r, 8), KVT_R8(r, 16), KVT_R8(r, 24)
+      : "r"(at));
+}
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+      "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::KVT_W8(r, 0),
+      KVT_W8(r, 8), KVT_W8(r, 16), KVT_W8(r, 24), "r"(at)
+      : "memory");
+}
+#define KVT_U8(r, i) "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7])
+// The loads are complete; what uses r comes behind.
+__device__ __forceinline__ void tmem_loaded(uint32_t* r) {
+  asm volatile("" : KVT_U8(r, 0), KVT_U8(r, 8));
+  asm volatile("" : KVT_U8(r, 16), KVT_U8(r, 24));
+}
+__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Operand in shared memory, 128-byte rows with the 128-byte swizzle: groups of eight rows 1,024 bytes apart;
+// `panels`: distance of the 64-element panels of an operand whose rows run along the product's sum
+// (V: a row is a token).
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t panels) {
+  return (uint64_t)((at >> 4) & 0x3fffu) | (uint64_t)((panels >> 4) & 0x3fffu) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// 32-bit accumulators, operands of T, M = 128; tr: B's rows run along the sum
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t instruction(uint32_t n, bool tr) {
+  const uint32_t type = sizeof(T) == 2 && std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  return 1u << 4 | type << 7 | type << 10 | (tr ? 1u : 0u) << 16 | (n >> 3) << 17 | (128u >> 4) << 24;
+}
+
+// Shapes.  kDk, kDv: elements of a key and of a value row; kCols: output columns of a CTA; kTok: tokens of a tile.
+template <int kDk_, int kDv_, int kCols_, int kTiles_, int kTok_, int kStages_>
+struct Shape {
+  static constexpr int kDk = kDk_, kDv = kDv_, kCols = kCols_, kTiles = kTiles_, kTok = kTok_, kStages = kStages_;
+  static constexpr bool kLatent = kDk != kDv;               // value rows lie in the key rows
+  static constexpr int kQTmem = kLatent ? 256 : 0;          // elements of Q in tensor memory
+  static constexpr int kQPanels = (kDk - kQTmem) / 64;
+  static constexpr int kPanelBytes = kTok * 128;
+  static constexpr int kKBytes = kDk / 64 * kPanelBytes, kVBytes = kLatent ? 0 : kDv / 64 * kPanelBytes;
+  static constexpr int kQBytes = kTiles * kQPanels * 128 * 128;
+  static constexpr int kMasks = kStages + 2;
+  static constexpr int kThreads = 64 + 128 * kTiles;
+  // tensor memory columns: outputs, then scores, then Q
+  static constexpr int kSlots = 2;                          // of scores: one for each row tile, or two in turn
+  static constexpr int kSAt = kTiles * kCols, kQAt = kSAt + kSlots * kTok;
+  static constexpr int kTmem = 512;
+  static_assert(kQAt + kQTmem / 2 <= kTmem, "tensor memory");
+  static constexpr int kControl = 1024;
+  static constexpr size_t kSmem = (size_t)kQBytes + kStages * (kKBytes + kVBytes) + kControl + 1024;
+};
+
+struct Control {   // in shared memory
+  unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4];
+  unsigned long long s_full[2], p_ready[2], pv_done[2];
+  uint32_t mask[8][4];
+  uint32_t tmem, gave_up;
+};
+static_assert(sizeof(Control) <= 1024, "control block");
+
+template <typename T, typename S>
+__global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
+                                                               uint32_t first_kind_items, uint32_t box_rows, uint32_t outside,
+                                                               uint32_t q_sign, uint32_t q_bits) {
+  constexpr int kHalves = S::kDv / S::kCols;   // CTAs that share out a row tile's columns
+  extern __shared__ uint8_t raw[];
+  uint8_t* const smem = raw + ((1024u - (smem_address(raw) & 1023u)) & 1023u);
+  uint8_t* const q_s = smem;
+  uint8_t* const ring = smem + S::kQBytes;
+  Control* const ctl = reinterpret_cast<Control*>(ring + S::kStages * (S::kKBytes + S::kVBytes));
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  wait_for_kernel_ahead();
+
+  Item w;
+  uint32_t i = blockIdx.x / kHalves;
+  const uint32_t col0 = blockIdx.x % kHalves * S::kCols;
+  const bool second = i >= first_kind_items;
+  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? i - first_kind_items : i, S::kTiles * 128, w, threadIdx.x == 0 && col0 == 0)) return;
+  if (w.to == 0) {
+    if (col0 == 0) put_nothing<T>(a, w);
+    return;
+  }
+  const int row_tiles = w.rows > 128u ? 2 : 1;
+  const TableView& tv = a.tv;
+  const uint32_t n_tiles = (w.to - w.from + S::kTok - 1u) / S::kTok;
+
+  if (threadIdx.x == 0) {
+    for (int b = 0; b < 4; ++b) {
+      bar_init(smem_address(&ctl->k_full[b]), 1);
+      bar_init(smem_address(&ctl->k_empty[b]), 1);
+      bar_init(smem_address(&ctl->v_full[b]), 1);
+      bar_init(smem_address(&ctl->v_empty[b]), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(smem_address(&ctl->s_full[b]), 1);
+      bar_init(smem_address(&ctl->p_ready[b]), 128);
+      bar_init(smem_address(&ctl->pv_done[b]), 1);
+    }
+    ctl->gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    proxy_fence();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl->tmem)), "r"(S::kTmem) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  // queries into shared memory, as the copies would lay them
+  for (uint32_t x = threadIdx.x; x < (uint32_t)row_tiles * 128u * (S::kQPanels * 8u); x += S::kThreads) {
+    const uint32_t r = x / (S::kQPanels * 8u), c = x % (S::kQPanels * 8u);
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < w.rows) {
+      uint32_t seq, head;
+      row_of(a, w, r, seq, head);
+      v = load8(static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + S::kQTmem + c * 8u);
+      v = make_uint4((v.x & q_bits) ^ q_sign, (v.y & q_bits) ^ q_sign, (v.z & q_bits) ^ q_sign, (v.w & q_bits) ^ q_sign);
+    }
+    *reinterpret_cast<uint4*>(q_s + ((r / 128u) * S::kQPanels + c / 8u) * 16384u + (r % 128u) * 128u + (((c % 8u) ^ (r & 7u)) * 16u)) = v;
+  }
+  proxy_fence();
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = ctl->tmem;
+  volatile uint32_t* const gave_up = &ctl->gave_up;
+  uint32_t* const status = tv.status;
+
+  if (S::kQTmem) {
+    // ... and the rest of them into tensor memory, a thread per row
+    if (warp >= 2) {
+      const uint32_t quarter = (uint32_t)(warp & 3) * 32u, row = quarter + lane;
+#pragma unroll 1
+      for (int c = 0; c < S::kQTmem / 64; ++c) {
+        uint32_t v[32];
+        uint32_t seq = 0, head = 0;
+        if (row < w.rows) row_of(a, w, row, seq, head);
+        const T* src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 64;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint4 x = row < w.rows ? load8(src + e * 8) : make_uint4(0, 0, 0, 0);
+          v[4 * e] = (x.x & q_bits) ^ q_sign;
+          v[4 * e + 1] = (x.y & q_bits) ^ q_sign;
+          v[4 * e + 2] = (x.z & q_bits) ^ q_sign;
+          v[4 * e + 3] = (x.w & q_bits) ^ q_sign;
+        }
+        tmem_store(tmem + (quarter << 16) + S::kQAt + c * 32, v);
+      }
+      tmem_wait_store();
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+  }
+
+  if (warp == 0) {
+    // ---- blocks ----
+    const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box;
+    auto look = [&](uint32_t t) {   // the chunk of the box that this lane copies
+      const uint32_t at = w.from + t * S::kTok + lane * rows_per_box;
+      return (uint32_t)lane < boxes && t < n_tiles && at < w.to ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(at), w.head) : ~0u;
+    };
+    uint32_t next = look(0);
+    bool ok = true;
+    for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+      const uint32_t st = t % S::kStages, round = t / S::kStages;
+      const uint32_t ch = next;
+      next = look(t + 1);
+      if (round) ok = bar_wait(smem_address(&ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
+      ok = __all_sync(~0u, ok);
+      if (!ok) break;
+      const uint32_t tile0 = w.from + t * S::kTok;
+#pragma unroll
+      for (int m = 0; m < S::kTok / 32; ++m) {
+        const uint32_t tok = m * 32 + lane;
+        const bool there = __shfl_sync(~0u, ch, tok / rows_per_box) != ~0u && tile0 + tok < w.to;
+        const uint32_t bits = __ballot_sync(~0u, there);
+        if (lane == 0) ctl->mask[t % S::kMasks][m] = bits;
+      }
+      uint8_t* const k_dst = ring + st * (S::kKBytes + S::kVBytes);
+      const uint32_t k_bar = smem_address(&ctl->k_full[st]);
+      if (lane == 0) bar_expect(k_bar, S::kKBytes);
+      __syncwarp();
+      const uint32_t at = tile0 + lane * rows_per_box;
+      const uint32_t in_block = at - tv.by_tokens(at) * tv.block_tokens;
+      const int32_t y = (int32_t)(ch != ~0u ? ch * tv.block_tokens + in_block : outside);
+      if ((uint32_t)lane < boxes)
+        for (int p = 0; p < S::kDk / 64; ++p)
+          tma_box(smem_address(k_dst) + p * S::kPanelBytes + lane * rows_per_box * 128u, &map, p * 64, y, k_bar);
+      if (!S::kLatent) {
+        if (round) ok = bar_wait(smem_address(&ctl->v_empty[st]), (round - 1) & 1, gave_up, status);
+        ok = __all_sync(~0u, ok);
+        if (!ok) break;
+        const uint32_t v_bar = smem_address(&ctl->v_full[st]);
+        if (lane == 0) bar_expect(v_bar, S::kVBytes);
+        __syncwarp();
+        const int32_t yv = ch != ~0u ? y + (int32_t)(tv.heads * tv.block_tokens) : y;
+        if ((uint32_t)lane < boxes)
+          for (int p = 0; p < S::kDv / 64; ++p)
+            tma_box(smem_address(k_dst + S::kKBytes) + p * S::kPanelBytes + lane * rows_per_box * 128u, &map, p * 64, yv, v_bar);
+      }
+    }
+  } else if (warp == 1) {
+    // ---- matrix instructions ----
+    if (lane == 0) {
+      const uint32_t q_at = smem_address(q_s), ring_at = smem_address(ring);
+      constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
+      auto scores = [&](uint32_t t, int r, int slot) {   // S[slot] = Q_r K_t^T
+        const uint32_t kt = ring_at + (t % S::kStages) * kStage;
+        const uint32_t d = tmem + S::kSAt + slot * S::kTok;
+        bool add = false;
+#pragma unroll
+        for (int k = 0; k < S::kQTmem / 16; ++k) {
+          mma_ts(d, tmem + S::kQAt + k * 8, operand(kt + (k / 4) * S::kPanelBytes + (k % 4) * 32, 0), instruction<T>(S::kTok, false), add);
+          add = true;
+        }
+#pragma unroll
+        for (int k = 0; k < S::kQPanels * 4; ++k) {
+          const int kk = k + S::kQTmem / 16;
+          mma_ss(d, operand(q_at + (r * S::kQPanels + k / 4) * 16384 + (k % 4) * 32, 0),
+                 operand(kt + (kk / 4) * S::kPanelBytes + (kk % 4) * 32, 0), instruction<T>(S::kTok, false), add);
+          add = true;
+        }
+        commit(smem_address(&ctl->s_full[slot]));
+      };
+      auto output = [&](uint32_t t, int r, int slot) {   // O_r += P[slot] V_t
+        const uint32_t vt = ring_at + (t % S::kStages) * kStage + (S::kLatent ? (col0 / 64) * S::kPanelBytes : S::kKBytes);
+#pragma unroll
+        for (int k = 0; k < S::kTok / 16; ++k)
+          mma_ts(tmem + r * S::kCols, tmem + S::kSAt + slot * S::kTok + k * 8, operand(vt + k * 2048, S::kPanelBytes),
+                 instruction<T>(S::kCols, true), t > 0 || k > 0);
+        commit(smem_address(&ctl->pv_done[r]));
+      };
+      auto wait_k = [&](uint32_t t) { return bar_wait(smem_address(&ctl->k_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status); };
+      auto wait_v = [&](uint32_t t) { return bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status); };
+      bool ok = wait_k(0);
+      if (ok) {
+        fence_after();
+        if (S::kTiles == 2) {
+          for (int r = 0; r < row_tiles; ++r) scores(0, r, r);
+          commit(smem_address(&ctl->k_empty[0]));
+          for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+            for (int r = 0; r < row_tiles && ok; ++r) {
+              ok = (r > 0 || wait_v(t)) && bar_wait(smem_address(&ctl->p_ready[r]), t & 1, gave_up, status);
+              if (!ok) break;
+              fence_after();
+              output(t, r, r);
+              if (r == row_tiles - 1) commit(smem_address(&ctl->v_empty[t % S::kStages]));
+              if (t + 1 < n_tiles) {
+                ok = r > 0 || wait_k(t + 1);
+                if (!ok) break;
+                fence_after();
+                scores(t + 1, r, r);
+                if (r == row_tiles - 1) commit(smem_address(&ctl->k_empty[(t + 1) % S::kStages]));
+              }
+            }
+          }
+        } else {
+          scores(0, 0, 0);
+          for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+            if (t + 1 < n_tiles) {
+              ok = wait_k(t + 1);
+              if (!ok) break;
+              fence_after();
+              scores(t + 1, 0, (t + 1) & 1);
+            }
+            ok = bar_wait(smem_address(&ctl->p_ready[t & 1]), (t >> 1) & 1, gave_up, status);
+            if (!ok) break;
+            fence_after();
+            output(t, 0, t & 1);
+            commit(smem_address(&ctl->k_empty[t % S::kStages]));
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // ---- softmax: a thread per row ----
+    const int r = (warp - 2) / 4;
+    const uint32_t lane_at = (uint32_t)(warp & 3) * 32u;   // a warp reaches the lanes of its number modulo four
+    const uint32_t row = r * 128u + lane_at + lane;
+    if (r < row_tiles) {
+      const bool mine = row < w.rows;
+      const uint32_t o_at = tmem + (lane_at << 16) + r * S::kCols;
+      float m = -INFINITY, l = 0.0f;
+      bool ok = true;
+      for (uint32_t t = 0; t < n_tiles; ++t) {
+        const int slot = S::kTiles == 2 ? r : (int)(t & 1);
+        const uint32_t turn = S::kTiles == 2 ? t : t >> 1;
+        const uint32_t s_at = tmem + (lane_at << 16) + S::kSAt + slot * S::kTok;
+        // (the tile's mask was written ahead of its copies)
+        ok = bar_wait(smem_address(&ctl->k_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status) &&
+             bar_wait(smem_address(&ctl->s_full[slot]), turn & 1, gave_up, status);
+        ok = __all_sync(~0u, ok);
+        if (!ok) break;
+        fence_after();
+        uint32_t bits[S::kTok];
+        float* const s = reinterpret_cast<float*>(bits);
+#pragma unroll
+        for (int c = 0; c < S::kTok / 32; ++c) tmem_load(bits + c * 32, s_at + c * 32);
+        tmem_wait_load();
+#pragma unroll
+        for (int c = 0; c < S::kTok / 32; ++c) tmem_loaded(bits + c * 32);
+        uint32_t mask[S::kTok / 32], all = ~0u;
+#pragma unroll
+        for (int c = 0; c < S::kTok / 32; ++c) {
+          mask[c] = ctl->mask[t % S::kMasks][c];
+          all &= mask[c];
+        }
+        if (all != ~0u) {
+#pragma unroll
+          for (int e = 0; e < S::kTok; ++e)
+            if (!(mask[e / 32] >> (e % 32) & 1u)) s[e] = -INFINITY;
+        }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int e = 0; e < S::kTok; e += 4) {
+          top[0] = fmaxf(top[0], s[e]);
+          top[1] = fmaxf(top[1], s[e + 1]);
+          top[2] = fmaxf(top[2], s[e + 2]);
+          top[3] = fmaxf(top[3], s[e + 3]);
+        }
+        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale2;
+        // the base follows the maximum when it has grown by 8 (or from nothing)
+        float turn_by = 1.0f;
+        if (mx > m + 8.0f || (m == -INFINITY && mx > m)) {
+          turn_by = exp2_(m - mx);
+          m = mx;
+          l *= turn_by;
+        }
+        const float base = m == -INFINITY ? 0.0f : m;
+        if (t > 0 && __any_sync(~0u, turn_by != 1.0f)) {
+          // (no product of this row tile is under way: the next waits for these probabilities)
+          ok = bar_wait(smem_address(&ctl->pv_done[r]), (t - 1) & 1, gave_up, status);
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
+          fence_after();
+#pragma unroll 1
+          for (int c = 0; c < S::kCols / 32; ++c) {
+            uint32_t o[32];
+            tmem_load(o, o_at + c * 32);
+            tmem_wait_load();
+            tmem_loaded(o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * turn_by);
+            tmem_store(o_at + c * 32, o);
+          }
+          tmem_wait_store();
+        }
+#pragma unroll
+        for (int g = 0; g < S::kTok / 16; ++g) {
+          float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+          for (int e = g * 16; e < g * 16 + 16; e += 2) {
+            const float x = exp2_(__fmaf_rn(s[e], a.scale2, -base)), y = exp2_(__fmaf_rn(s[e + 1], a.scale2, -base));
+            sum[0] += x;
+            sum[1] += y;
+            bits[e / 2] = pack2<T>(x, y);
+          }
+          const float both = sum[0] + sum[1];
+          l += both;
+          if (a.weight && mine && w.from + t * S::kTok + g * 16u < w.to)
+            grain_at(a, w, (w.from + t * S::kTok) / 16u + g)[row] = base + log2_(both);
+        }
+#pragma unroll
+        for (int c = 0; c < S::kTok / 64; ++c) tmem_store(s_at + c * 32, bits + c * 32);
+        tmem_wait_store();
+        // what lies behind the last token, in its block, would meet probabilities of zero: it may be anything
+        const uint32_t left = w.to - (w.from + t * S::kTok);
+        if (left < (uint32_t)S::kTok && left % box_rows) {
+          if (!S::kLatent) {
+            ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
+            ok = __all_sync(~0u, ok);
+            if (!ok) break;
+          }
+          uint8_t* const vt = ring + (t % S::kStages) * (S::kKBytes + S::kVBytes) + (S::kLatent ? 0 : S::kKBytes);
+          const uint32_t end = (left + box_rows - 1u) / box_rows * box_rows;
+          for (uint32_t x = lane_at + lane; x < (end - left) * (S::kDv / 8u); x += 128u) {
+            const uint32_t tok = left + x / (S::kDv / 8u), c = x % (S::kDv / 8u);
+            *reinterpret_cast<uint4*>(vt + (c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+          }
+          proxy_fence();
+        }
+        fence_before();
+        bar_arrive(smem_address(&ctl->p_ready[slot]));
+      }
+      if (ok) ok = bar_wait(smem_address(&ctl->pv_done[r]), (n_tiles - 1) & 1, gave_up, status);
+      ok = __all_sync(~0u, ok);
+      if (ok) {
+        fence_after();
+        uint32_t seq = 0, head = 0;
+        if (mine) row_of(a, w, row, seq, head);
+        const uint32_t part = part_of(a, w);
+        const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < S::kCols / 32; ++c) {
+          uint32_t o[32];
+          tmem_load(o, o_at + c * 32);
+          tmem_wait_load();
+          tmem_loaded(o);
+          if (!mine) continue;
+          if (a.direct) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 2)
+              put2<T>(a, seq, head, part, col0 + c * 32 + e, __uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
+          } else {
+            float* const to = a.part_o + (((uint64_t)seq * a.q_heads + head) * a.n_parts + part) * a.dv + col0 + c * 32;
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4*>(to + e) = make_float4(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv,
+                                                               __uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+          }
+        }
+        if (mine && col0 == 0) put_lse(a, seq, head, part, l != 0.0f ? m + log2_(l) : -INFINITY);
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  if (warp == 1) {
+    if (ctl->gave_up) {
+      // copies and products in flight end before the memory is given back
+      if (lane == 0) {
+        commit(smem_address(&ctl->pv_done[0]));
+        for (uint32_t k = 0; k < 1u << 16; ++k) asm volatile("nanosleep.u32 1000;");
+      }
+      __syncwarp();
+    }
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kTmem));
+  }
+}
+
+typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                           const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder (its address does not change while the process runs).
+Encode encoder() {
+  static const Encode f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<Encode>(p);
+  }();
+  return f;
+}
+
+template <typename T, typename S>
+cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s) {
+  const TableView& tv = a.tv;
+  const uint32_t box = tv.block_tokens < (uint32_t)S::kTok ? tv.block_tokens : (uint32_t)S::kTok;
+  const uint64_t rows = tv.n * tv.n_chunks * tv.block_tokens;
+  CUtensorMap map;
+  const cuuint64_t dims[2] = {(cuuint64_t)S::kDk, rows}, strides[1] = {(cuuint64_t)S::kDk * 2};
+  const cuuint32_t box_dims[2] = {64, box}, steps[2] = {1, 1};
+  if (encoder()(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, tv.slab, dims, strides, box_dims, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  const uint64_t tile = S::kTiles * 128;
+  const uint64_t np = prefix ? ((uint64_t)a.max_members * a.group + tile - 1) / tile * a.chunks[0] * tv.heads * a.n_groups : 0;
+  const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
+  const uint64_t grid = (np + ns) * (S::kDv / S::kCols);
+  if (grid == 0) return cudaSuccess;
+  if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
+  auto* kernel = tiles_kernel<T, S>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
+  if (e != cudaSuccess) return e;
+  AttendArgs b = a;
+  // the base follows the largest product, and what is masked is -inf before it is scaled: a negative scale
+  // turns the queries around instead, a scale of 0 makes them zeros
+  uint32_t sign = 0, bits = ~0u;
+  if (b.scale2 < 0.0f) {
+    b.scale2 = -b.scale2;
+    sign = 0x80008000u;
+  } else if (b.scale2 == 0.0f) {
+    b.scale2 = 1.0f;
+    bits = 0;
+  }
+  return launch_overlapped_smem(kernel, (unsigned)grid, (unsigned)S::kThreads, S::kSmem, s, b, map, (uint32_t)np, box, (uint32_t)rows, sign, bits);
+}
+
+using Heads128 = Shape<128, 128, 128, 2, 128, 2>;
+using Heads64 = Shape<64, 64, 64, 2, 128, 4>;
+using Latents = Shape<576, 512, 256, 1, 64, 2>;
+
+template <typename T>
+cudaError_t launch_typed(const AttendArgs& a, bool mla, bool prefix, bool suffix, cudaStream_t s) {
+  if (mla) return launch<T, Latents>(a, prefix, suffix, s);
+  return a.dk == 128 ? launch<T, Heads128>(a, prefix, suffix, s) : launch<T, Heads64>(a, prefix, suffix, s);
+}
+
+}  // namespace
+
+bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows, bool weights) {
+  const uint32_t tok = mla ? Latents::kTok : Heads128::kTok;
+  if (mla ? dk != 576 || dv != 512 : dk != 128 && dk != 64) return false;
+  if (block_tokens % 8 != 0 || (tok % block_tokens != 0 && block_tokens % tok != 0)) return false;
+  if (weights && block_tokens % 16 != 0) return false;   // (they are kept by 16 tokens)
+  // (a box's place is a signed number of rows)
+  return slab_rows < 0x7fff0000ull && encoder() != nullptr;
+}
+
+cudaError_t launch_attend_tiles(const AttendArgs& a, int dtype, bool mla, bool prefix, bool suffix, cudaStream_t s) {
+  return dtype == KV_DTYPE_BF16 ? launch_typed<__nv_bfloat16>(a, mla, prefix, suffix, s) : launch_typed<__half>(a, mla, prefix, suffix, s);
+}
+
+}  // namespace kvt

@@ -45,45 +45,66 @@ TableView table_view(const PoolView& v, int32_t q, int32_t layer, const uint32_t
 }
 
 // How a call's work is split: tokens of a chunk and chunks, for prefixes and suffixes.
+constexpr uint32_t kSms = 148;
+// Rows from which on a segment goes to the tensor cores' 128-row tiles.
+constexpr uint32_t kTileRows = 48;
 struct Split {
+  bool tiles[2];
   uint32_t chunk_tokens[2], chunks[2], n_parts, grain_tokens, grains[2];
   uint64_t lse_at, grain_at[2], bytes;
 };
 
-// Chunks of a segment: enough CTAs for two full turns of the SMs (two resident on each), as long as a
-// chunk keeps 128 tokens.
-void split_segment(uint64_t ctas, uint32_t most, uint32_t block_tokens, uint32_t* chunk, uint32_t* chunks) {
-  const uint64_t target = 148u * 4u;
-  const uint64_t want = ctas ? (target + ctas - 1) / ctas : 1;
-  uint64_t c = ((uint64_t)most + want - 1) / want;
-  c = (c + 63) / 64 * 64;
-  if (c < 128) c = 128;
-  uint64_t limit = (uint64_t)kMaxChunkBlocks * block_tokens / 64 * 64;
-  if (limit < 64) limit = 64;
+// Chunks of a segment of `most` tokens when `ctas` row tiles are split alike and `slots` CTAs run at a time: the
+// split whose turns, times the tiles of a chunk and what a CTA costs beside them (`extra` tiles), are fewest.
+void split_segment(uint64_t ctas, uint32_t most, uint32_t tile, uint32_t slots, uint32_t extra, uint32_t block_tokens, uint32_t* chunk,
+                   uint32_t* chunks) {
+  uint64_t limit = (uint64_t)kMaxChunkBlocks * block_tokens / tile * tile;
+  if (limit < tile) limit = tile;
   if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
-  if (c > limit) c = limit;
-  *chunk = (uint32_t)c;
-  *chunks = (uint32_t)(((uint64_t)most + c - 1) / c);
+  if (!ctas) ctas = 1;
+  const uint64_t tiles = ((uint64_t)most + tile - 1) / tile, most_tiles = limit / tile;
+  uint64_t n = (tiles + most_tiles - 1) / most_tiles, best = ~0ull, best_tiles = 1;
+  const uint64_t last = n + 2 * slots / ctas + 1;
+  for (; n <= last && n <= tiles; ++n) {
+    const uint64_t per = (tiles + n - 1) / n, parts = (tiles + per - 1) / per;
+    const uint64_t cost = (ctas * parts + slots - 1) / slots * (per + extra);
+    if (cost < best) {
+      best = cost;
+      best_tiles = per;
+    }
+  }
+  *chunk = (uint32_t)(best_tiles * tile);
+  *chunks = (uint32_t)((tiles + best_tiles - 1) / best_tiles);
 }
 
-bool split(const PoolView& v, int32_t q, uint32_t dv, uint32_t n_seqs, uint32_t n_groups, uint32_t max_suffix,
+bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_seqs, uint32_t n_groups, uint32_t max_suffix,
            uint32_t max_prefix, uint32_t max_members, bool weights, Split* out) {
   const uint32_t bt = (uint32_t)v.desc->part[q].block_tokens, heads = v.geom[q].heads;
   const uint32_t q_heads = (uint32_t)v.desc->part[q].model.n_q_heads, group = q_heads / heads;
   const bool mla = v.variant[q] == KV_MLA;
-  const uint32_t tile = mla ? 64u : 16u;
   const bool shared = n_groups && max_prefix && max_members;
   // (per token of the longest run nothing may leave 31 bits)
   if (max_suffix >= 0x40000000u || max_prefix >= 0x40000000u || n_seqs >= 0x1000000u || n_groups >= 0x1000000u) return false;
   if (max_members > n_seqs) max_members = n_seqs;
   if ((uint64_t)max_members * group >= 0x10000000u || (uint64_t)n_seqs * q_heads >= 0x40000000u) return false;
+  out->tiles[0] = out->tiles[1] = false;
   out->chunk_tokens[0] = out->chunk_tokens[1] = 64;
   out->chunks[0] = out->chunks[1] = 0;
   const uint64_t prefix_rows = (uint64_t)max_members * group;
-  const uint64_t row_tile = mla ? 64 : prefix_rows <= 16 ? 16 : prefix_rows <= 32 ? 32 : 64;
-  if (shared)
-    split_segment((prefix_rows + row_tile - 1) / row_tile * heads * n_groups, max_prefix, bt, &out->chunk_tokens[0], &out->chunks[0]);
-  split_segment((uint64_t)((group + tile - 1) / tile) * heads * n_seqs, max_suffix ? max_suffix : 1, bt, &out->chunk_tokens[1], &out->chunks[1]);
+  const bool fits = tiles_take(dk, dv, mla, bt, v.geom[q].n * v.geom[q].n_chunks * bt, weights);
+  for (int k = 0; k < 2; ++k) {
+    if (k == 0 && !shared) continue;
+    const uint64_t rows = k == 0 ? prefix_rows : group, segs = (uint64_t)(k == 0 ? n_groups : n_seqs) * heads;
+    const uint32_t most = k == 0 ? max_prefix : max_suffix ? max_suffix : 1;
+    out->tiles[k] = fits && rows >= kTileRows;
+    if (out->tiles[k]) {
+      const uint64_t tile = mla ? 128 : 256;
+      split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, mla ? 64 : 128, kSms, 4, bt, &out->chunk_tokens[k], &out->chunks[k]);
+    } else {
+      const uint64_t tile = mla ? 64 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+      split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, bt, &out->chunk_tokens[k], &out->chunks[k]);
+    }
+  }
   out->n_parts = out->chunks[0] + out->chunks[1];
   out->grain_tokens = bt % 16 == 0 ? 16 : 1;
   const unsigned __int128 rows = (unsigned __int128)n_seqs * q_heads;
@@ -119,7 +140,7 @@ uint64_t kv_attend_scratch_bytes(kv_pool* p, int32_t q, uint32_t n_seqs, uint32_
   uint32_t dk, dv;
   if (q < 0 || q >= v.n_parts || dims(v, q, &dk, &dv) != KV_OK || !attend_dims(v, q, dk, dv)) return 0;
   Split s;
-  return split(v, q, dv, n_seqs, n_groups, max_suffix, max_prefix, max_members, weights != 0, &s) ? (s.bytes ? s.bytes : 256) : 0;
+  return split(v, q, dk, dv, n_seqs, n_groups, max_suffix, max_prefix, max_members, weights != 0, &s) ? (s.bytes ? s.bytes : 256) : 0;
 }
 
 int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
@@ -139,7 +160,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   if (d->n_rows && (!d->d_table || !aligned(d->d_table, 4))) return KV_ERR_INVALID_ARG;
   if (d->n_rows >= 0x100000000ull || !aligned(d->d_lse, 4) || !aligned(d->d_weight, 8)) return KV_ERR_INVALID_ARG;
   Split sp;
-  if (!split(v, q, dv, d->n_seqs, d->n_groups, d->max_suffix, d->max_prefix, d->max_members, d->d_weight != nullptr, &sp)) return KV_ERR_INVALID_ARG;
+  if (!split(v, q, dk, dv, d->n_seqs, d->n_groups, d->max_suffix, d->max_prefix, d->max_members, d->d_weight != nullptr, &sp)) return KV_ERR_INVALID_ARG;
   if (!d->d_scratch || !aligned(d->d_scratch, 16) || d->scratch_bytes < sp.bytes) return KV_ERR_INVALID_ARG;
   const int32_t rs = pool_settle(p, stream);
   if (rs != KV_OK) return rs;
@@ -167,6 +188,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   a.max_members = d->max_members < d->n_seqs ? d->max_members : d->n_seqs;
   uint8_t* const scratch = static_cast<uint8_t*>(d->d_scratch);
   for (int k = 0; k < 2; ++k) {
+    a.tiles[k] = sp.tiles[k];
     a.chunk_tokens[k] = sp.chunk_tokens[k];
     a.chunks[k] = sp.chunks[k];
     a.grains[k] = sp.grains[k];

@@ -119,6 +119,26 @@ __device__ __forceinline__ void tmem_loaded(uint32_t* r) {
 __device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Two 32-bit operations in one instruction.
+struct Pair {
+  unsigned long long v;
+  __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+  __device__ __forceinline__ void get(float& lo, float& hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+};
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(a.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return a;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(a.v) : "l"(a.v), "l"(b.v));
+  return a;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
 // Operand in shared memory, 128-byte rows with the 128-byte swizzle: groups of eight rows 1,024 bytes apart;
 // `panels`: distance of the 64-element panels of an operand whose rows run along the product's sum
 // (V: a row is a token).
@@ -139,11 +159,15 @@ struct Shape {
   static constexpr bool kLatent = kDk != kDv;               // value rows lie in the key rows
   static constexpr int kQTmem = kLatent ? 256 : 0;          // elements of Q in tensor memory
   static constexpr int kQPanels = (kDk - kQTmem) / 64;
-  static constexpr int kPanelBytes = kTok * 128;
-  static constexpr int kKBytes = kDk / 64 * kPanelBytes, kVBytes = kLatent ? 0 : kDv / 64 * kPanelBytes;
+  static constexpr int kPanelBytes = kTok * 128;            // a tile's tokens x 64 elements
+  // A stage has two parts that are filled and given back on their own: keys and values, or (MLA) the panels that only
+  // the scores read and the CTA's columns of the values, which the scores read too.
+  static constexpr int kAPanels = kLatent ? (kDk - kCols) / 64 : kDk / 64, kBPanels = kCols / 64;
+  static constexpr int kKBytes = kAPanels * kPanelBytes, kVBytes = kBPanels * kPanelBytes;
   static constexpr int kQBytes = kTiles * kQPanels * 128 * 128;
   static constexpr int kMasks = kStages + 2;
-  static constexpr int kThreads = 64 + 128 * kTiles;
+  static constexpr int kFirst = kTiles == 2 ? 4 : 2;        // first warp of the softmax
+  static constexpr int kThreads = (kFirst + 4 * kTiles) * 32;
   // tensor memory columns: outputs, then scores, then Q
   static constexpr int kSlots = 2;                          // of scores: one for each row tile, or two in turn
   static constexpr int kSAt = kTiles * kCols, kQAt = kSAt + kSlots * kTok;
@@ -160,6 +184,14 @@ struct Control {   // in shared memory
   uint32_t tmem, gave_up;
 };
 static_assert(sizeof(Control) <= 1024, "control block");
+
+// First element of panel p of a stage's part.
+template <typename S>
+__device__ __forceinline__ int panel_at(int part, int p, uint32_t col0) {
+  if (!S::kLatent) return p * 64;
+  if (part) return (int)col0 + p * 64;
+  return p * 64 + (p * 64 >= (int)col0 ? S::kCols : 0);
+}
 
 template <typename T, typename S>
 __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
@@ -229,7 +261,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
 
   if (S::kQTmem) {
     // ... and the rest of them into tensor memory, a thread per row
-    if (warp >= 2) {
+    if (warp >= S::kFirst) {
       const uint32_t quarter = (uint32_t)(warp & 3) * 32u, row = quarter + lane;
 #pragma unroll 1
       for (int c = 0; c < S::kQTmem / 64; ++c) {
@@ -256,76 +288,79 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
 
   if (warp == 0) {
     // ---- blocks ----
-    const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box;
-    auto look = [&](uint32_t t) {   // the chunk of the box that this lane copies
-      const uint32_t at = w.from + t * S::kTok + lane * rows_per_box;
-      return (uint32_t)lane < boxes && t < n_tiles && at < w.to ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(at), w.head) : ~0u;
+    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // boxes of a tile; the lanes look the blocks of 32 of them up at a time, before they are needed
+    const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box, ahead = 32u / boxes;
+    auto look = [&](uint32_t t) {   // of tiles t .. t + ahead - 1: the chunk of box lane % boxes of tile t + lane / boxes
+      const uint32_t box = t * boxes + lane, at = w.from + box * rows_per_box;
+      return (uint32_t)lane < boxes * ahead && at < w.to ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(at), w.head) : ~0u;
     };
-    uint32_t next = look(0);
+    uint32_t next = look(0), now = ~0u;
     bool ok = true;
     for (uint32_t t = 0; t < n_tiles && ok; ++t) {
       const uint32_t st = t % S::kStages, round = t / S::kStages;
-      const uint32_t ch = next;
-      next = look(t + 1);
-      if (round) ok = bar_wait(smem_address(&ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
-      ok = __all_sync(~0u, ok);
-      if (!ok) break;
+      if (t % ahead == 0) {
+        now = next;
+        if (t + ahead < n_tiles) next = look(t + ahead);
+      }
+      const uint32_t first = t % ahead * boxes;
+      const uint32_t ch = __shfl_sync(~0u, now, first + lane % boxes);
       const uint32_t tile0 = w.from + t * S::kTok;
+      uint32_t bits[S::kTok / 32];
 #pragma unroll
       for (int m = 0; m < S::kTok / 32; ++m) {
         const uint32_t tok = m * 32 + lane;
-        const bool there = __shfl_sync(~0u, ch, tok / rows_per_box) != ~0u && tile0 + tok < w.to;
-        const uint32_t bits = __ballot_sync(~0u, there);
-        if (lane == 0) ctl->mask[t % S::kMasks][m] = bits;
+        bits[m] = __ballot_sync(~0u, __shfl_sync(~0u, ch, tok / rows_per_box) != ~0u && tile0 + tok < w.to);
       }
-      uint8_t* const k_dst = ring + st * (S::kKBytes + S::kVBytes);
-      const uint32_t k_bar = smem_address(&ctl->k_full[st]);
-      if (lane == 0) bar_expect(k_bar, S::kKBytes);
-      __syncwarp();
       const uint32_t at = tile0 + lane * rows_per_box;
       const uint32_t in_block = at - tv.by_tokens(at) * tv.block_tokens;
       const int32_t y = (int32_t)(ch != ~0u ? ch * tv.block_tokens + in_block : outside);
-      if ((uint32_t)lane < boxes)
-        for (int p = 0; p < S::kDk / 64; ++p)
-          tma_box(smem_address(k_dst) + p * S::kPanelBytes + lane * rows_per_box * 128u, &map, p * 64, y, k_bar);
-      if (!S::kLatent) {
-        if (round) ok = bar_wait(smem_address(&ctl->v_empty[st]), (round - 1) & 1, gave_up, status);
+      uint8_t* const k_dst = ring + st * (S::kKBytes + S::kVBytes);
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        if (round) ok = bar_wait(smem_address(part ? &ctl->v_empty[st] : &ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
         ok = __all_sync(~0u, ok);
         if (!ok) break;
-        const uint32_t v_bar = smem_address(&ctl->v_full[st]);
-        if (lane == 0) bar_expect(v_bar, S::kVBytes);
+        const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
+        if (lane == 0) {
+          if (part == 0) {
+#pragma unroll
+            for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
+          }
+          bar_expect(bar, part ? S::kVBytes : S::kKBytes);
+        }
         __syncwarp();
-        const int32_t yv = ch != ~0u ? y + (int32_t)(tv.heads * tv.block_tokens) : y;
+        const int32_t yp = part && !S::kLatent && ch != ~0u ? y + (int32_t)(tv.heads * tv.block_tokens) : y;
+        const uint32_t dst = smem_address(k_dst) + (part ? S::kKBytes : 0) + lane * rows_per_box * 128u;
         if ((uint32_t)lane < boxes)
-          for (int p = 0; p < S::kDv / 64; ++p)
-            tma_box(smem_address(k_dst + S::kKBytes) + p * S::kPanelBytes + lane * rows_per_box * 128u, &map, p * 64, yv, v_bar);
+          for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p)
+            tma_box(dst + p * S::kPanelBytes, &map, panel_at<S>(part, p, col0), yp, bar);
       }
     }
   } else if (warp == 1) {
     // ---- matrix instructions ----
+    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (lane == 0) {
       const uint32_t q_at = smem_address(q_s), ring_at = smem_address(ring);
       constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
-      auto scores = [&](uint32_t t, int r, int slot) {   // S[slot] = Q_r K_t^T
-        const uint32_t kt = ring_at + (t % S::kStages) * kStage;
+      // S[slot] (+)= Q_r K_t^T over the elements of a stage's part
+      auto scores = [&](uint32_t t, int r, int slot, int part) {
+        const uint32_t kt = ring_at + (t % S::kStages) * kStage + (part ? S::kKBytes : 0);
         const uint32_t d = tmem + S::kSAt + slot * S::kTok;
-        bool add = false;
 #pragma unroll
-        for (int k = 0; k < S::kQTmem / 16; ++k) {
-          mma_ts(d, tmem + S::kQAt + k * 8, operand(kt + (k / 4) * S::kPanelBytes + (k % 4) * 32, 0), instruction<T>(S::kTok, false), add);
-          add = true;
-        }
+        for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p) {
+          const int at = panel_at<S>(part, p, col0);
 #pragma unroll
-        for (int k = 0; k < S::kQPanels * 4; ++k) {
-          const int kk = k + S::kQTmem / 16;
-          mma_ss(d, operand(q_at + (r * S::kQPanels + k / 4) * 16384 + (k % 4) * 32, 0),
-                 operand(kt + (kk / 4) * S::kPanelBytes + (kk % 4) * 32, 0), instruction<T>(S::kTok, false), add);
-          add = true;
+          for (int k = 0; k < 4; ++k) {
+            const uint64_t b = operand(kt + p * S::kPanelBytes + k * 32, 0);
+            const bool add = part || p || k;
+            if (at < S::kQTmem) mma_ts(d, tmem + S::kQAt + at / 2 + k * 8, b, instruction<T>(S::kTok, false), add);
+            else mma_ss(d, operand(q_at + (r * S::kQPanels + (at - S::kQTmem) / 64) * 16384 + k * 32, 0), b, instruction<T>(S::kTok, false), add);
+          }
         }
-        commit(smem_address(&ctl->s_full[slot]));
       };
       auto output = [&](uint32_t t, int r, int slot) {   // O_r += P[slot] V_t
-        const uint32_t vt = ring_at + (t % S::kStages) * kStage + (S::kLatent ? (col0 / 64) * S::kPanelBytes : S::kKBytes);
+        const uint32_t vt = ring_at + (t % S::kStages) * kStage + S::kKBytes;
 #pragma unroll
         for (int k = 0; k < S::kTok / 16; ++k)
           mma_ts(tmem + r * S::kCols, tmem + S::kSAt + slot * S::kTok + k * 8, operand(vt + k * 2048, S::kPanelBytes),
@@ -334,50 +369,64 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       };
       auto wait_k = [&](uint32_t t) { return bar_wait(smem_address(&ctl->k_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status); };
       auto wait_v = [&](uint32_t t) { return bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status); };
-      bool ok = wait_k(0);
-      if (ok) {
+      bool ok = true;
+      if (S::kTiles == 2) {
+        ok = wait_k(0);
         fence_after();
-        if (S::kTiles == 2) {
-          for (int r = 0; r < row_tiles; ++r) scores(0, r, r);
-          commit(smem_address(&ctl->k_empty[0]));
-          for (uint32_t t = 0; t < n_tiles && ok; ++t) {
-            for (int r = 0; r < row_tiles && ok; ++r) {
-              ok = (r > 0 || wait_v(t)) && bar_wait(smem_address(&ctl->p_ready[r]), t & 1, gave_up, status);
-              if (!ok) break;
-              fence_after();
-              output(t, r, r);
-              if (r == row_tiles - 1) commit(smem_address(&ctl->v_empty[t % S::kStages]));
-              if (t + 1 < n_tiles) {
-                ok = r > 0 || wait_k(t + 1);
-                if (!ok) break;
-                fence_after();
-                scores(t + 1, r, r);
-                if (r == row_tiles - 1) commit(smem_address(&ctl->k_empty[(t + 1) % S::kStages]));
-              }
-            }
+        if (ok) {
+          for (int r = 0; r < row_tiles; ++r) {
+            scores(0, r, r, 0);
+            commit(smem_address(&ctl->s_full[r]));
           }
-        } else {
-          scores(0, 0, 0);
-          for (uint32_t t = 0; t < n_tiles && ok; ++t) {
-            if (t + 1 < n_tiles) {
-              ok = wait_k(t + 1);
-              if (!ok) break;
-              fence_after();
-              scores(t + 1, 0, (t + 1) & 1);
-            }
-            ok = bar_wait(smem_address(&ctl->p_ready[t & 1]), (t >> 1) & 1, gave_up, status);
+          commit(smem_address(&ctl->k_empty[0]));
+        }
+        for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+          for (int r = 0; r < row_tiles && ok; ++r) {
+            ok = (r > 0 || wait_v(t)) && bar_wait(smem_address(&ctl->p_ready[r]), t & 1, gave_up, status);
             if (!ok) break;
             fence_after();
-            output(t, 0, t & 1);
-            commit(smem_address(&ctl->k_empty[t % S::kStages]));
+            output(t, r, r);
+            if (r == row_tiles - 1) commit(smem_address(&ctl->v_empty[t % S::kStages]));
+            if (t + 1 < n_tiles) {
+              ok = r > 0 || wait_k(t + 1);
+              if (!ok) break;
+              fence_after();
+              scores(t + 1, r, r, 0);
+              commit(smem_address(&ctl->s_full[r]));
+              if (r == row_tiles - 1) commit(smem_address(&ctl->k_empty[(t + 1) % S::kStages]));
+            }
           }
+        }
+      } else {
+        auto both = [&](uint32_t t) {
+          if (!wait_k(t)) return false;
+          fence_after();
+          scores(t, 0, t & 1, 0);
+          commit(smem_address(&ctl->k_empty[t % S::kStages]));
+          if (!wait_v(t)) return false;
+          fence_after();
+          scores(t, 0, t & 1, 1);
+          commit(smem_address(&ctl->s_full[t & 1]));
+          return true;
+        };
+        ok = both(0);
+        for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+          if (t + 1 < n_tiles) ok = both(t + 1);
+          ok = ok && bar_wait(smem_address(&ctl->p_ready[t & 1]), (t >> 1) & 1, gave_up, status);
+          if (!ok) break;
+          fence_after();
+          output(t, 0, t & 1);
+          commit(smem_address(&ctl->v_empty[t % S::kStages]));
         }
       }
     }
     __syncwarp();
+  } else if (warp < S::kFirst) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   } else {
     // ---- softmax: a thread per row ----
-    const int r = (warp - 2) / 4;
+    if (S::kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");   // 128 x (72 + 2 x 216) of 384 x 168
+    const int r = (warp - S::kFirst) / 4;
     const uint32_t lane_at = (uint32_t)(warp & 3) * 32u;   // a warp reaches the lanes of its number modulo four
     const uint32_t row = r * 128u + lane_at + lane;
     if (r < row_tiles) {
@@ -413,14 +462,14 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
           for (int e = 0; e < S::kTok; ++e)
             if (!(mask[e / 32] >> (e % 32) & 1u)) s[e] = -INFINITY;
         }
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-        for (int e = 0; e < S::kTok; e += 4) {
-          top[0] = fmaxf(top[0], s[e]);
-          top[1] = fmaxf(top[1], s[e + 1]);
-          top[2] = fmaxf(top[2], s[e + 2]);
-          top[3] = fmaxf(top[3], s[e + 3]);
+        for (int e = 4; e + 8 <= S::kTok; e += 8) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[e + 2 * k], s[e + 2 * k + 1]);
         }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], s[S::kTok - 4 + k]);
         const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale2;
         // the base follows the maximum when it has grown by 8 (or from nothing)
         float turn_by = 1.0f;
@@ -430,6 +479,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
           l *= turn_by;
         }
         const float base = m == -INFINITY ? 0.0f : m;
+        const Pair scale(a.scale2, a.scale2), minus(-base, -base);
         if (t > 0 && __any_sync(~0u, turn_by != 1.0f)) {
           // (no product of this row tile is under way: the next waits for these probabilities)
           ok = bar_wait(smem_address(&ctl->pv_done[r]), (t - 1) & 1, gave_up, status);
@@ -450,17 +500,21 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         }
 #pragma unroll
         for (int g = 0; g < S::kTok / 16; ++g) {
-          float sum[2] = {0.0f, 0.0f};
+          Pair sum(0.0f, 0.0f);
 #pragma unroll
           for (int e = g * 16; e < g * 16 + 16; e += 2) {
-            const float x = exp2_(__fmaf_rn(s[e], a.scale2, -base)), y = exp2_(__fmaf_rn(s[e + 1], a.scale2, -base));
-            sum[0] += x;
-            sum[1] += y;
+            float x, y;
+            fma2(Pair(s[e], s[e + 1]), scale, minus).get(x, y);
+            x = exp2_(x);
+            y = exp2_(y);
+            sum = add2(sum, Pair(x, y));
             bits[e / 2] = pack2<T>(x, y);
           }
-          const float both = sum[0] + sum[1];
+          float lo, hi;
+          sum.get(lo, hi);
+          const float both = lo + hi;
           l += both;
-          if (a.weight && mine && w.from + t * S::kTok + g * 16u < w.to)
+          if (a.weight && mine && col0 == 0 && w.from + t * S::kTok + g * 16u < w.to)
             grain_at(a, w, (w.from + t * S::kTok) / 16u + g)[row] = base + log2_(both);
         }
 #pragma unroll
@@ -469,15 +523,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         // what lies behind the last token, in its block, would meet probabilities of zero: it may be anything
         const uint32_t left = w.to - (w.from + t * S::kTok);
         if (left < (uint32_t)S::kTok && left % box_rows) {
-          if (!S::kLatent) {
-            ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
-            ok = __all_sync(~0u, ok);
-            if (!ok) break;
-          }
-          uint8_t* const vt = ring + (t % S::kStages) * (S::kKBytes + S::kVBytes) + (S::kLatent ? 0 : S::kKBytes);
+          ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
+          uint8_t* const vt = ring + (t % S::kStages) * (S::kKBytes + S::kVBytes) + S::kKBytes;
           const uint32_t end = (left + box_rows - 1u) / box_rows * box_rows;
-          for (uint32_t x = lane_at + lane; x < (end - left) * (S::kDv / 8u); x += 128u) {
-            const uint32_t tok = left + x / (S::kDv / 8u), c = x % (S::kDv / 8u);
+          for (uint32_t x = lane_at + lane; x < (end - left) * (S::kCols / 8u); x += 128u) {
+            const uint32_t tok = left + x / (S::kCols / 8u), c = x % (S::kCols / 8u);
             *reinterpret_cast<uint4*>(vt + (c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
           }
           proxy_fence();

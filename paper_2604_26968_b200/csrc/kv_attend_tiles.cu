@@ -27,7 +27,7 @@
 namespace kvt {
 namespace {
 
-constexpr unsigned long long kWaitLimit = 2'000'000'000ull;   // nanoseconds
+constexpr long long kWaitLimit = 4'000'000'000ll;   // cycles of the SM: about two seconds
 
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -52,15 +52,11 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 // False: this wait, or another of the CTA, has given up.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t* status) {
   if (bar_try(bar, parity)) return true;
-  unsigned long long from, now;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(from));
+  const long long from = clock64();
   do {
-    for (int i = 0; i < 64; ++i) {
-      if (bar_try(bar, parity)) return true;
-      if (*gave_up) return false;
-    }
-    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-  } while (now - from < kWaitLimit);
+    if (bar_try(bar, parity)) return true;
+    if (*gave_up) return false;
+  } while (clock64() - from < kWaitLimit);
   *gave_up = 1u;
   atomicOr(status, KV_DEV_WAIT_EXPIRED);
   return false;
@@ -77,21 +73,29 @@ __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::aft
 __device__ __forceinline__ void commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// An operand's descriptor: the lower half moves with the address, the upper half is the same for all (see operand()).
+constexpr uint32_t kOperandHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
 // D (+)= A B, A and B from shared memory
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kOperandHigh)
       : "memory");
 }
 // A from tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\tsetp.ne.u32 p, %4, 0;\n\tmov.b64 y, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kOperandHigh)
       : "memory");
+}
+// One thread of the warp.
+__device__ __forceinline__ bool elected() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+  return r != 0;
 }
 #define KVT_R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define KVT_W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
@@ -139,12 +143,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Operand in shared memory, 128-byte rows with the 128-byte swizzle: groups of eight rows 1,024 bytes apart;
-// `panels`: distance of the 64-element panels of an operand whose rows run along the product's sum
-// (V: a row is a token).
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t panels) {
-  return (uint64_t)((at >> 4) & 0x3fffu) | (uint64_t)((panels >> 4) & 0x3fffu) << 16 | (uint64_t)(1024u >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// Operand in shared memory, 128-byte rows with the 128-byte swizzle: groups of eight rows 1,024 bytes apart
+// (the upper half); `panels`: distance of the 64-element panels of an operand whose rows run along the
+// product's sum (V: a row is a token).
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t panels) { return (at >> 4) | (panels >> 4) << 16; }
 // 32-bit accumulators, operands of T, M = 128; tr: B's rows run along the sum
 template <typename T>
 __device__ __forceinline__ constexpr uint32_t instruction(uint32_t n, bool tr) {
@@ -169,7 +171,7 @@ struct Shape {
   static constexpr int kFirst = kTiles == 2 ? 4 : 2;        // first warp of the softmax
   static constexpr int kThreads = (kFirst + 4 * kTiles) * 32;
   // tensor memory columns: outputs, then scores, then Q
-  static constexpr int kSlots = 2;                          // of scores: one for each row tile, or two in turn
+  static constexpr int kSlots = 2 * kTiles;                 // of scores: two for each row tile, in turn
   static constexpr int kSAt = kTiles * kCols, kQAt = kSAt + kSlots * kTok;
   static constexpr int kTmem = 512;
   static_assert(kQAt + kQTmem / 2 <= kTmem, "tensor memory");
@@ -179,7 +181,7 @@ struct Shape {
 
 struct Control {   // in shared memory
   unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4];
-  unsigned long long s_full[2], p_ready[2], pv_done[2];
+  unsigned long long s_full[4], p_ready[4], pv_done[2];
   uint32_t mask[8][4];
   uint32_t tmem, gave_up;
 };
@@ -187,10 +189,86 @@ static_assert(sizeof(Control) <= 1024, "control block");
 
 // First element of panel p of a stage's part.
 template <typename S>
-__device__ __forceinline__ int panel_at(int part, int p, uint32_t col0) {
-  if (!S::kLatent) return p * 64;
-  if (part) return (int)col0 + p * 64;
-  return p * 64 + (p * 64 >= (int)col0 ? S::kCols : 0);
+__host__ __device__ constexpr int panel_at(int part, int p, int col0) {
+  return !S::kLatent ? p * 64 : part ? col0 + p * 64 : p * 64 + (p * 64 >= col0 ? S::kCols : 0);
+}
+
+// The products of a CTA.  While the probabilities of tile t are formed, the scores of tile t + 1 are.
+template <typename T, typename S, int kCol0>
+__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int row_tiles_, uint32_t n_tiles_,
+                                      uint32_t* status) {
+  constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
+  constexpr uint32_t kScores = instruction<T>(S::kTok, false), kOutput = instruction<T>(S::kCols, true);
+  volatile uint32_t* const gave_up = &ctl->gave_up;
+  // (the same for the whole warp, so that addresses and descriptors stay in uniform registers)
+  const uint32_t tmem = __shfl_sync(~0u, tmem_, 0), n_tiles = __shfl_sync(~0u, n_tiles_, 0);
+  const int row_tiles = __shfl_sync(~0u, row_tiles_, 0);
+  // S_r[t & 1] (+)= Q_r K_t^T over the elements of a stage's part
+  auto scores = [&](uint32_t t, int r, int part) {
+    const uint32_t k_op = operand(ring_at + (t % S::kStages) * kStage + (part ? S::kKBytes : 0), 0);
+    const uint32_t q_op = operand(q_at + r * (S::kQPanels * 16384), 0);
+    const uint32_t d = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok;
+#pragma unroll
+    for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p) {
+      const int at = panel_at<S>(part, p, kCol0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t b = k_op + (p * S::kPanelBytes + k * 32) / 16, add = part || p || k;
+        if (at < S::kQTmem) mma_ts(d, tmem + S::kQAt + at / 2 + k * 8, b, kScores, add);
+        else mma_ss(d, q_op + ((at - S::kQTmem) / 64 * 16384 + k * 32) / 16, b, kScores, add);
+      }
+    }
+  };
+  auto output = [&](uint32_t t, int r) {   // O_r += P_r[t & 1] V_t
+    const uint32_t v_op = operand(ring_at + (t % S::kStages) * kStage + S::kKBytes, S::kPanelBytes);
+    const uint32_t p_at = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok, o_at = tmem + r * S::kCols;
+#pragma unroll
+    for (int k = 0; k < S::kTok / 16; ++k) mma_ts(o_at, p_at + k * 8, v_op + k * 128, kOutput, k ? 1u : t);
+  };
+  auto wait = [&](unsigned long long* bar, uint32_t parity) {
+    const bool ok = __all_sync(~0u, bar_wait(smem_address(bar), parity, gave_up, status));
+    fence_after();
+    return ok;
+  };
+  auto next_scores = [&](uint32_t t) {
+    const uint32_t st = t % S::kStages, parity = (t / S::kStages) & 1;
+    if (!wait(&ctl->k_full[st], parity)) return false;
+    for (int r = 0; r < row_tiles; ++r) {
+      // these scores take the place of probabilities that an output of two tiles ago is formed from: products of
+      // different accumulators may overlap, so it has to be complete
+      if (t >= 2 && !wait(&ctl->pv_done[r], t & 1)) return false;
+      if (elected()) {
+        scores(t, r, 0);
+        if (!S::kLatent) commit(smem_address(&ctl->s_full[2 * r + (t & 1)]));
+        if (r == row_tiles - 1) commit(smem_address(&ctl->k_empty[st]));
+      }
+      __syncwarp();
+    }
+    if (S::kLatent) {
+      if (!wait(&ctl->v_full[st], parity)) return false;
+      if (elected()) {
+        scores(t, 0, 1);
+        commit(smem_address(&ctl->s_full[t & 1]));
+      }
+      __syncwarp();
+    }
+    return true;
+  };
+  if (!next_scores(0)) return;
+  for (uint32_t t = 0; t < n_tiles; ++t) {
+    if (t + 1 < n_tiles && !next_scores(t + 1)) return;
+    const uint32_t st = t % S::kStages;
+    if (!S::kLatent && !wait(&ctl->v_full[st], (t / S::kStages) & 1)) return;
+    for (int r = 0; r < row_tiles; ++r) {
+      if (!wait(&ctl->p_ready[2 * r + (t & 1)], (t >> 1) & 1)) return;
+      if (elected()) {
+        output(t, r);
+        commit(smem_address(&ctl->pv_done[r]));
+        if (r == row_tiles - 1) commit(smem_address(&ctl->v_empty[st]));
+      }
+      __syncwarp();
+    }
+  }
 }
 
 template <typename T, typename S>
@@ -225,12 +303,10 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       bar_init(smem_address(&ctl->k_empty[b]), 1);
       bar_init(smem_address(&ctl->v_full[b]), 1);
       bar_init(smem_address(&ctl->v_empty[b]), 1);
-    }
-    for (int b = 0; b < 2; ++b) {
       bar_init(smem_address(&ctl->s_full[b]), 1);
       bar_init(smem_address(&ctl->p_ready[b]), 128);
-      bar_init(smem_address(&ctl->pv_done[b]), 1);
     }
+    for (int b = 0; b < 2; ++b) bar_init(smem_address(&ctl->pv_done[b]), 1);
     ctl->gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     proxy_fence();
@@ -323,7 +399,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         if (!ok) break;
         const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
         if (lane == 0) {
-          if (part == 0) {
+          if (part == 1) {   // (the softmax reads it behind v_full, and v_empty says that it has)
 #pragma unroll
             for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
           }
@@ -338,89 +414,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       }
     }
   } else if (warp == 1) {
-    // ---- matrix instructions ----
+    // ---- matrix instructions: the whole warp waits, one thread issues ----
     if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (lane == 0) {
-      const uint32_t q_at = smem_address(q_s), ring_at = smem_address(ring);
-      constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
-      // S[slot] (+)= Q_r K_t^T over the elements of a stage's part
-      auto scores = [&](uint32_t t, int r, int slot, int part) {
-        const uint32_t kt = ring_at + (t % S::kStages) * kStage + (part ? S::kKBytes : 0);
-        const uint32_t d = tmem + S::kSAt + slot * S::kTok;
-#pragma unroll
-        for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p) {
-          const int at = panel_at<S>(part, p, col0);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint64_t b = operand(kt + p * S::kPanelBytes + k * 32, 0);
-            const bool add = part || p || k;
-            if (at < S::kQTmem) mma_ts(d, tmem + S::kQAt + at / 2 + k * 8, b, instruction<T>(S::kTok, false), add);
-            else mma_ss(d, operand(q_at + (r * S::kQPanels + (at - S::kQTmem) / 64) * 16384 + k * 32, 0), b, instruction<T>(S::kTok, false), add);
-          }
-        }
-      };
-      auto output = [&](uint32_t t, int r, int slot) {   // O_r += P[slot] V_t
-        const uint32_t vt = ring_at + (t % S::kStages) * kStage + S::kKBytes;
-#pragma unroll
-        for (int k = 0; k < S::kTok / 16; ++k)
-          mma_ts(tmem + r * S::kCols, tmem + S::kSAt + slot * S::kTok + k * 8, operand(vt + k * 2048, S::kPanelBytes),
-                 instruction<T>(S::kCols, true), t > 0 || k > 0);
-        commit(smem_address(&ctl->pv_done[r]));
-      };
-      auto wait_k = [&](uint32_t t) { return bar_wait(smem_address(&ctl->k_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status); };
-      auto wait_v = [&](uint32_t t) { return bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status); };
-      bool ok = true;
-      if (S::kTiles == 2) {
-        ok = wait_k(0);
-        fence_after();
-        if (ok) {
-          for (int r = 0; r < row_tiles; ++r) {
-            scores(0, r, r, 0);
-            commit(smem_address(&ctl->s_full[r]));
-          }
-          commit(smem_address(&ctl->k_empty[0]));
-        }
-        for (uint32_t t = 0; t < n_tiles && ok; ++t) {
-          for (int r = 0; r < row_tiles && ok; ++r) {
-            ok = (r > 0 || wait_v(t)) && bar_wait(smem_address(&ctl->p_ready[r]), t & 1, gave_up, status);
-            if (!ok) break;
-            fence_after();
-            output(t, r, r);
-            if (r == row_tiles - 1) commit(smem_address(&ctl->v_empty[t % S::kStages]));
-            if (t + 1 < n_tiles) {
-              ok = r > 0 || wait_k(t + 1);
-              if (!ok) break;
-              fence_after();
-              scores(t + 1, r, r, 0);
-              commit(smem_address(&ctl->s_full[r]));
-              if (r == row_tiles - 1) commit(smem_address(&ctl->k_empty[(t + 1) % S::kStages]));
-            }
-          }
-        }
-      } else {
-        auto both = [&](uint32_t t) {
-          if (!wait_k(t)) return false;
-          fence_after();
-          scores(t, 0, t & 1, 0);
-          commit(smem_address(&ctl->k_empty[t % S::kStages]));
-          if (!wait_v(t)) return false;
-          fence_after();
-          scores(t, 0, t & 1, 1);
-          commit(smem_address(&ctl->s_full[t & 1]));
-          return true;
-        };
-        ok = both(0);
-        for (uint32_t t = 0; t < n_tiles && ok; ++t) {
-          if (t + 1 < n_tiles) ok = both(t + 1);
-          ok = ok && bar_wait(smem_address(&ctl->p_ready[t & 1]), (t >> 1) & 1, gave_up, status);
-          if (!ok) break;
-          fence_after();
-          output(t, 0, t & 1);
-          commit(smem_address(&ctl->v_empty[t % S::kStages]));
-        }
-      }
-    }
-    __syncwarp();
+    if (S::kDv == S::kCols) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), row_tiles, n_tiles, status);
+    else if (col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), row_tiles, n_tiles, status);
+    else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), row_tiles, n_tiles, status);
   } else if (warp < S::kFirst) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
   } else {
@@ -435,12 +433,11 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       float m = -INFINITY, l = 0.0f;
       bool ok = true;
       for (uint32_t t = 0; t < n_tiles; ++t) {
-        const int slot = S::kTiles == 2 ? r : (int)(t & 1);
-        const uint32_t turn = S::kTiles == 2 ? t : t >> 1;
+        const int slot = 2 * r + (int)(t & 1);
         const uint32_t s_at = tmem + (lane_at << 16) + S::kSAt + slot * S::kTok;
-        // (the tile's mask was written ahead of its copies)
-        ok = bar_wait(smem_address(&ctl->k_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status) &&
-             bar_wait(smem_address(&ctl->s_full[slot]), turn & 1, gave_up, status);
+        // (the tile's mask was written ahead of the copies of its second part)
+        ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status) &&
+             bar_wait(smem_address(&ctl->s_full[slot]), (t >> 1) & 1, gave_up, status);
         ok = __all_sync(~0u, ok);
         if (!ok) break;
         fence_after();
@@ -523,9 +520,6 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         // what lies behind the last token, in its block, would meet probabilities of zero: it may be anything
         const uint32_t left = w.to - (w.from + t * S::kTok);
         if (left < (uint32_t)S::kTok && left % box_rows) {
-          ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
-          ok = __all_sync(~0u, ok);
-          if (!ok) break;
           uint8_t* const vt = ring + (t % S::kStages) * (S::kKBytes + S::kVBytes) + S::kKBytes;
           const uint32_t end = (left + box_rows - 1u) / box_rows * box_rows;
           for (uint32_t x = lane_at + lane; x < (end - left) * (S::kCols / 8u); x += 128u) {
@@ -537,6 +531,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         fence_before();
         bar_arrive(smem_address(&ctl->p_ready[slot]));
       }
+      // (the last product but one may not be complete either, and a wait tells no two phases apart that lie two apart)
+      if (ok && n_tiles > 1) ok = bar_wait(smem_address(&ctl->pv_done[r]), (n_tiles - 2) & 1, gave_up, status);
       if (ok) ok = bar_wait(smem_address(&ctl->pv_done[r]), (n_tiles - 1) & 1, gave_up, status);
       ok = __all_sync(~0u, ok);
       if (ok) {
@@ -635,8 +631,8 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s
   return launch_overlapped_smem(kernel, (unsigned)grid, (unsigned)S::kThreads, S::kSmem, s, b, map, (uint32_t)np, box, (uint32_t)rows, sign, bits);
 }
 
-using Heads128 = Shape<128, 128, 128, 2, 128, 2>;
-using Heads64 = Shape<64, 64, 64, 2, 128, 4>;
+using Heads128 = Shape<128, 128, 128, 2, 64, 4>;
+using Heads64 = Shape<64, 64, 64, 2, 64, 4>;
 using Latents = Shape<576, 512, 256, 1, 64, 2>;
 
 template <typename T>

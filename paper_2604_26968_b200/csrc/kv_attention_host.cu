@@ -99,7 +99,7 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
     out->tiles[k] = fits && rows >= kTileRows;
     if (out->tiles[k]) {
       const uint64_t tile = mla ? 128 : 256;
-      split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, mla ? 64 : 128, kSms, 4, bt, &out->chunk_tokens[k], &out->chunks[k]);
+      split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, bt, &out->chunk_tokens[k], &out->chunks[k]);
     } else {
       const uint64_t tile = mla ? 64 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
       split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, bt, &out->chunk_tokens[k], &out->chunks[k]);

@@ -6,7 +6,7 @@
 // of tokens lies in shared memory as the matrix instructions want it whatever blocks it is made of; a block
 // that is not there is a box outside the tensor, which reads as zeros.
 //
-// Roles: warp 0 looks blocks up and issues the copies, one thread of warp 1 issues the matrix
+// Roles: warp 0 looks blocks up and issues the copies, a warp for each row tile issues its matrix
 // instructions, and each further group of four warps is a row tile's softmax, a thread per row: it reads its row
 // of S, keeps maximum and sum, and writes the probabilities over S, from where P V takes them as the operand
 // in tensor memory.  With two row tiles (kTiles == 2) the tensor cores work on one's products while the
@@ -181,7 +181,7 @@ struct Shape {
 
 struct Control {   // in shared memory
   unsigned long long k_full[4], k_empty[4], v_full[4], v_empty[4];
-  unsigned long long s_full[4], p_ready[4], pv_done[2];
+  unsigned long long s_full[4], p_ready[4], pv_done[2], o_done[2], q_ready[2];
   uint32_t mask[8][4];
   uint32_t tmem, gave_up;
 };
@@ -193,20 +193,19 @@ __host__ __device__ constexpr int panel_at(int part, int p, int col0) {
   return !S::kLatent ? p * 64 : part ? col0 + p * 64 : p * 64 + (p * 64 >= col0 ? S::kCols : 0);
 }
 
-// The products of a CTA.  While the probabilities of tile t are formed, the scores of tile t + 1 are.
+// The products of row tile r.  While the probabilities of tile t are formed, the scores of tile t + 1 are.
 template <typename T, typename S, int kCol0>
-__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int row_tiles_, uint32_t n_tiles_,
-                                      uint32_t* status) {
+__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int r_, uint32_t n_tiles_, uint32_t* status) {
   constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
   constexpr uint32_t kScores = instruction<T>(S::kTok, false), kOutput = instruction<T>(S::kCols, true);
   volatile uint32_t* const gave_up = &ctl->gave_up;
   // (the same for the whole warp, so that addresses and descriptors stay in uniform registers)
   const uint32_t tmem = __shfl_sync(~0u, tmem_, 0), n_tiles = __shfl_sync(~0u, n_tiles_, 0);
-  const int row_tiles = __shfl_sync(~0u, row_tiles_, 0);
+  const int r = __shfl_sync(~0u, r_, 0);
+  const uint32_t q_op = operand(q_at + r * (S::kQPanels * 16384), 0), o_at = tmem + r * S::kCols;
   // S_r[t & 1] (+)= Q_r K_t^T over the elements of a stage's part
-  auto scores = [&](uint32_t t, int r, int part) {
+  auto scores = [&](uint32_t t, int part) {
     const uint32_t k_op = operand(ring_at + (t % S::kStages) * kStage + (part ? S::kKBytes : 0), 0);
-    const uint32_t q_op = operand(q_at + r * (S::kQPanels * 16384), 0);
     const uint32_t d = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok;
 #pragma unroll
     for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p) {
@@ -219,56 +218,107 @@ __device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_a
       }
     }
   };
-  auto output = [&](uint32_t t, int r) {   // O_r += P_r[t & 1] V_t
+  auto output = [&](uint32_t t) {   // O_r += P_r[t & 1] V_t
     const uint32_t v_op = operand(ring_at + (t % S::kStages) * kStage + S::kKBytes, S::kPanelBytes);
-    const uint32_t p_at = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok, o_at = tmem + r * S::kCols;
+    const uint32_t p_at = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok;
 #pragma unroll
     for (int k = 0; k < S::kTok / 16; ++k) mma_ts(o_at, p_at + k * 8, v_op + k * 128, kOutput, k ? 1u : t);
   };
   auto wait = [&](unsigned long long* bar, uint32_t parity) {
-    const bool ok = __all_sync(~0u, bar_wait(smem_address(bar), parity, gave_up, status));
-    fence_after();
-    return ok;
+    return __all_sync(~0u, bar_wait(smem_address(bar), parity, gave_up, status));
   };
   auto next_scores = [&](uint32_t t) {
     const uint32_t st = t % S::kStages, parity = (t / S::kStages) & 1;
     if (!wait(&ctl->k_full[st], parity)) return false;
-    for (int r = 0; r < row_tiles; ++r) {
-      // these scores take the place of probabilities that an output of two tiles ago is formed from: products of
-      // different accumulators may overlap, so it has to be complete
-      if (t >= 2 && !wait(&ctl->pv_done[r], t & 1)) return false;
-      if (elected()) {
-        scores(t, r, 0);
-        if (!S::kLatent) commit(smem_address(&ctl->s_full[2 * r + (t & 1)]));
-        if (r == row_tiles - 1) commit(smem_address(&ctl->k_empty[st]));
-      }
-      __syncwarp();
+    // these scores take the place of probabilities that an output of two tiles ago is formed from: products of
+    // different accumulators may overlap, so it has to be complete
+    if (t >= 2 && !wait(&ctl->pv_done[r], t & 1)) return false;
+    fence_after();
+    if (elected()) {
+      scores(t, 0);
+      if (!S::kLatent) commit(smem_address(&ctl->s_full[2 * r + (t & 1)]));
+      commit(smem_address(&ctl->k_empty[st]));
     }
+    __syncwarp();
     if (S::kLatent) {
       if (!wait(&ctl->v_full[st], parity)) return false;
       if (elected()) {
-        scores(t, 0, 1);
+        scores(t, 1);
         commit(smem_address(&ctl->s_full[t & 1]));
       }
       __syncwarp();
     }
     return true;
   };
+  if (!wait(&ctl->q_ready[r], 0)) return;
+  fence_after();
   if (!next_scores(0)) return;
   for (uint32_t t = 0; t < n_tiles; ++t) {
     if (t + 1 < n_tiles && !next_scores(t + 1)) return;
     const uint32_t st = t % S::kStages;
     if (!S::kLatent && !wait(&ctl->v_full[st], (t / S::kStages) & 1)) return;
-    for (int r = 0; r < row_tiles; ++r) {
-      if (!wait(&ctl->p_ready[2 * r + (t & 1)], (t >> 1) & 1)) return;
-      if (elected()) {
-        output(t, r);
-        commit(smem_address(&ctl->pv_done[r]));
-        if (r == row_tiles - 1) commit(smem_address(&ctl->v_empty[st]));
-      }
-      __syncwarp();
+    if (!wait(&ctl->p_ready[2 * r + (t & 1)], (t >> 1) & 1)) return;
+    fence_after();
+    if (elected()) {
+      output(t);
+      commit(smem_address(&ctl->pv_done[r]));
+      commit(smem_address(&ctl->v_empty[st]));
+      if (t + 1 == n_tiles) commit(smem_address(&ctl->o_done[r]));
+    }
+    __syncwarp();
+  }
+}
+
+// Rows of a row tile's queries into shared memory, as the copies would lay them, and (MLA) their first elements
+// into tensor memory, by the tile's 128 threads.
+template <typename T, typename S>
+__device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w, uint8_t* q_s, uint32_t tmem, int r, uint32_t thread, uint32_t lane_at,
+                                             uint32_t q_sign, uint32_t q_bits) {
+  auto source = [&](uint32_t row) {
+    uint32_t seq, head;
+    row_of(a, w, row, seq, head);
+    return static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head;
+  };
+  auto turned = [&](uint4 v) { return make_uint4((v.x & q_bits) ^ q_sign, (v.y & q_bits) ^ q_sign, (v.z & q_bits) ^ q_sign, (v.w & q_bits) ^ q_sign); };
+  constexpr int kVecs = S::kQPanels * 8;    // 16-byte vectors of a row
+  constexpr int kBatch = 8;
+#pragma unroll 1
+  for (int k0 = 0; k0 < kVecs; k0 += kBatch) {
+    uint4 v[kBatch];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const uint32_t x = thread + (k0 + k) * 128u, row = x / kVecs, c = x % kVecs;
+      v[k] = make_uint4(0, 0, 0, 0);
+      if (r * 128u + row < w.rows) v[k] = load8(source(r * 128u + row) + S::kQTmem + c * 8u);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const uint32_t x = thread + (k0 + k) * 128u, row = x / kVecs, c = x % kVecs;
+      *reinterpret_cast<uint4*>(q_s + (r * S::kQPanels + c / 8u) * 16384u + row * 128u + (((c % 8u) ^ (row & 7u)) * 16u)) = turned(v[k]);
     }
   }
+  if (S::kQTmem) {
+    const uint32_t row = lane_at + (thread & 31u);
+    const T* const src = source(row < w.rows ? row : 0u);
+#pragma unroll 1
+    for (int c = 0; c < S::kQTmem / 64; ++c) {
+      uint32_t v[32];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (row < w.rows) x = load8(src + c * 64 + e * 8);
+        x = turned(x);
+        v[4 * e] = x.x;
+        v[4 * e + 1] = x.y;
+        v[4 * e + 2] = x.z;
+        v[4 * e + 3] = x.w;
+      }
+      tmem_store(tmem + (lane_at << 16) + S::kQAt + c * 32, v);
+    }
+    tmem_wait_store();
+  }
+  proxy_fence();
+  fence_before();
 }
 
 template <typename T, typename S>
@@ -300,13 +350,17 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   if (threadIdx.x == 0) {
     for (int b = 0; b < 4; ++b) {
       bar_init(smem_address(&ctl->k_full[b]), 1);
-      bar_init(smem_address(&ctl->k_empty[b]), 1);
+      bar_init(smem_address(&ctl->k_empty[b]), row_tiles);
       bar_init(smem_address(&ctl->v_full[b]), 1);
-      bar_init(smem_address(&ctl->v_empty[b]), 1);
+      bar_init(smem_address(&ctl->v_empty[b]), row_tiles);
       bar_init(smem_address(&ctl->s_full[b]), 1);
       bar_init(smem_address(&ctl->p_ready[b]), 128);
     }
-    for (int b = 0; b < 2; ++b) bar_init(smem_address(&ctl->pv_done[b]), 1);
+    for (int b = 0; b < 2; ++b) {
+      bar_init(smem_address(&ctl->pv_done[b]), 1);
+      bar_init(smem_address(&ctl->o_done[b]), 1);
+      bar_init(smem_address(&ctl->q_ready[b]), 128);
+    }
     ctl->gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     proxy_fence();
@@ -315,52 +369,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&ctl->tmem)), "r"(S::kTmem) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  // queries into shared memory, as the copies would lay them
-  for (uint32_t x = threadIdx.x; x < (uint32_t)row_tiles * 128u * (S::kQPanels * 8u); x += S::kThreads) {
-    const uint32_t r = x / (S::kQPanels * 8u), c = x % (S::kQPanels * 8u);
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (r < w.rows) {
-      uint32_t seq, head;
-      row_of(a, w, r, seq, head);
-      v = load8(static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + S::kQTmem + c * 8u);
-      v = make_uint4((v.x & q_bits) ^ q_sign, (v.y & q_bits) ^ q_sign, (v.z & q_bits) ^ q_sign, (v.w & q_bits) ^ q_sign);
-    }
-    *reinterpret_cast<uint4*>(q_s + ((r / 128u) * S::kQPanels + c / 8u) * 16384u + (r % 128u) * 128u + (((c % 8u) ^ (r & 7u)) * 16u)) = v;
-  }
-  proxy_fence();
   fence_before();
   __syncthreads();
   fence_after();
   const uint32_t tmem = ctl->tmem;
   volatile uint32_t* const gave_up = &ctl->gave_up;
   uint32_t* const status = tv.status;
-
-  if (S::kQTmem) {
-    // ... and the rest of them into tensor memory, a thread per row
-    if (warp >= S::kFirst) {
-      const uint32_t quarter = (uint32_t)(warp & 3) * 32u, row = quarter + lane;
-#pragma unroll 1
-      for (int c = 0; c < S::kQTmem / 64; ++c) {
-        uint32_t v[32];
-        uint32_t seq = 0, head = 0;
-        if (row < w.rows) row_of(a, w, row, seq, head);
-        const T* src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + c * 64;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint4 x = row < w.rows ? load8(src + e * 8) : make_uint4(0, 0, 0, 0);
-          v[4 * e] = (x.x & q_bits) ^ q_sign;
-          v[4 * e + 1] = (x.y & q_bits) ^ q_sign;
-          v[4 * e + 2] = (x.z & q_bits) ^ q_sign;
-          v[4 * e + 3] = (x.w & q_bits) ^ q_sign;
-        }
-        tmem_store(tmem + (quarter << 16) + S::kQAt + c * 32, v);
-      }
-      tmem_wait_store();
-    }
-    fence_before();
-    __syncthreads();
-    fence_after();
-  }
 
   if (warp == 0) {
     // ---- blocks ----
@@ -413,14 +427,14 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
             tma_box(dst + p * S::kPanelBytes, &map, panel_at<S>(part, p, col0), yp, bar);
       }
     }
-  } else if (warp == 1) {
-    // ---- matrix instructions: the whole warp waits, one thread issues ----
-    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (S::kDv == S::kCols) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), row_tiles, n_tiles, status);
-    else if (col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), row_tiles, n_tiles, status);
-    else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), row_tiles, n_tiles, status);
   } else if (warp < S::kFirst) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    // ---- matrix instructions: a warp for each row tile; the whole warp waits, one thread issues ----
+    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    const int r = warp - 1;
+    if (r < row_tiles) {
+      if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, n_tiles, status);
+      else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, n_tiles, status);
+    }
   } else {
     // ---- softmax: a thread per row ----
     if (S::kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");   // 128 x (72 + 2 x 216) of 384 x 168
@@ -430,6 +444,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     if (r < row_tiles) {
       const bool mine = row < w.rows;
       const uint32_t o_at = tmem + (lane_at << 16) + r * S::kCols;
+      load_queries<T, S>(a, w, q_s, tmem, r, threadIdx.x - (S::kFirst + 4 * r) * 32, lane_at, q_sign, q_bits);
+      bar_arrive(smem_address(&ctl->q_ready[r]));
       float m = -INFINITY, l = 0.0f;
       bool ok = true;
       for (uint32_t t = 0; t < n_tiles; ++t) {
@@ -531,9 +547,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         fence_before();
         bar_arrive(smem_address(&ctl->p_ready[slot]));
       }
-      // (the last product but one may not be complete either, and a wait tells no two phases apart that lie two apart)
-      if (ok && n_tiles > 1) ok = bar_wait(smem_address(&ctl->pv_done[r]), (n_tiles - 2) & 1, gave_up, status);
-      if (ok) ok = bar_wait(smem_address(&ctl->pv_done[r]), (n_tiles - 1) & 1, gave_up, status);
+      if (ok) ok = bar_wait(smem_address(&ctl->o_done[r]), 0, gave_up, status);
       ok = __all_sync(~0u, ok);
       if (ok) {
         fence_after();

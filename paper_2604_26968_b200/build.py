@@ -12,7 +12,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvtier.so")
 SOURCES = ["kvtier_host.cu", "kv_attention_host.cu", "kv_score.cu", "kv_select.cu", "kv_select_persist.cu", "kv_blocks.cu", "kv_heads.cu", "kv_prefetch.cu", "kv_dedup.cu", "kv_move.cu", "kv_move_tma.cu",
-           "kv_append.cu", "kv_attend.cu", "kv_attend_tiles.cu", "kv_attention.cu"]
+           "kv_append.cu", "kv_attend.cu", "kv_attend_tiles.cu", "kv_attend_stream.cu", "kv_attention.cu"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

@@ -7,7 +7,7 @@
 // KV head -- of all members of a group, where it is a prefix -- are the rows of one small matrix product
 // per block, so that a block's K and V leave HBM once for all of them.  A segment's tokens are cut into
 // chunks that different CTAs work on; a part (one row, one chunk) is its normalised output and the log2 of
-// its sum of exponentials, and join_kernel adds the parts up with weights 2^(lse_part - lse).
+// its sum of exponentials, and finish_kernel adds the parts up with weights 2^(lse_part - lse).
 #include "kv_attend_device.cuh"
 
 namespace kvt {
@@ -22,39 +22,6 @@ template <int N>
 __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr));
-}
-__device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-               : "r"(addr));
-}
-template <typename T>
-__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
-template <>
-__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-template <>
-__device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ float quad_max(float x) {
-  x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
-  return fmaxf(x, __shfl_xor_sync(~0u, x, 2));
-}
-__device__ __forceinline__ float quad_sum(float x) {
-  x += __shfl_xor_sync(~0u, x, 1);
-  return x + __shfl_xor_sync(~0u, x, 2);
-}
-
 constexpr int kTile = 64;   // tokens of a tile
 
 // Rows of up to 256 elements.  kM x kN warps: kM share out the rows (16 each), kN the tokens of a tile
@@ -272,45 +239,10 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
     }
     return;
   }
-  // the warps of a row join: maxima and sums, then outputs
   copy_wait<0>();
   __syncthreads();
-  float* const o_s = reinterpret_cast<float*>(smem);                          // [kN][16 kM][D]
-  float* const ml_s = o_s + kN * kM * 16 * D;                                 // [kN][16 kM][2]
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = wm * 16 + lane / 4 + h * 8;
-    if ((lane & 3) == 0) {
-      ml_s[(wn * kM * 16 + r) * 2] = m[h];
-      ml_s[(wn * kM * 16 + r) * 2 + 1] = l[h];
-    }
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j)
-      *reinterpret_cast<float2*>(o_s + (wn * kM * 16 + r) * D + ((j ^ (r & 7)) * 8 + (lane & 3) * 2)) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
-  }
-  __syncthreads();
-  for (uint32_t i = threadIdx.x; i < kM * 16 * (D / 2); i += kThreadsHere) {
-    const uint32_t r = i / (D / 2), d = i % (D / 2) * 2u;
-    if (r >= w.rows || d >= a.dv) continue;
-    float top = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < kN; ++n) top = fmaxf(top, ml_s[(n * kM * 16 + r) * 2]);
-    const float from = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll
-    for (int n = 0; n < kN; ++n) {
-      const float c = exp2_(ml_s[(n * kM * 16 + r) * 2] - from);
-      const float2 v = *reinterpret_cast<const float2*>(o_s + (n * kM * 16 + r) * D + (((d / 8u) ^ (r & 7u)) * 8u + d % 8u));
-      sum += c * ml_s[(n * kM * 16 + r) * 2 + 1];
-      x += c * v.x;
-      y += c * v.y;
-    }
-    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-    uint32_t seq, head;
-    row_of(a, w, r, seq, head);
-    put2<T>(a, seq, head, part, d, x * inv, y * inv);
-    if (d == 0) put_lse(a, seq, head, part, sum != 0.0f ? top + log2_(sum) : -INFINITY);
-  }
+  join_warps<D, kM, kN>(smem, wm, wn, o, m, l);
+  put_joined<T, D, kM, kN>(a, w, part, smem);
 }
 
 // MLA: one row per token is key (all dk elements) and value (the first dv) of every query head.  kM x kN warps:
@@ -533,113 +465,160 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
   }
 }
 
-// ---- parts to outputs: a warp per (sequence, query head) -----------------------------------------
+// ---- parts to outputs, grains to weights -------------------------------------------------------------
 
-constexpr int kJoinThreads = 128;
+constexpr int kFinishThreads = 256, kFinishRows = kFinishThreads / 32;
+constexpr uint32_t kWeightBlocks = 64, kWeightRows = 1024;   // blocks of a CTA, rows whose sums it holds at a time
 
+// The parts of a sequence: np of its group's prefix, ns of its suffix, the latter behind the places of all prefix chunks.
+struct Parts {
+  uint32_t np, ns, suffix_at;
+  __device__ __forceinline__ uint32_t place(uint32_t i) const { return i < np ? i : suffix_at + i - np; }
+};
+__device__ __forceinline__ Parts parts_of(const AttendArgs& a, uint32_t seq) {
+  Parts p{0, 0, a.chunks[0]};
+  const Segment sfx = a.checked(a.suffix, seq, a.max_suffix, false);
+  if (a.n_groups) {
+    const uint32_t g = a.group_of(seq);
+    if (g != ~0u) p.np = (a.checked(a.prefix, g, a.max_prefix, false).tokens + a.chunk_tokens[0] - 1u) / a.chunk_tokens[0];
+  }
+  p.ns = (sfx.tokens + a.chunk_tokens[1] - 1u) / a.chunk_tokens[1];
+  return p;
+}
+
+// out and lse of rows (sequence, query head), a warp for each.
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendArgs a) {
-  wait_for_kernel_ahead();
-  const uint64_t row = (uint64_t)blockIdx.x * (kJoinThreads / 32) + threadIdx.x / 32;
+__device__ __forceinline__ void join_rows(const AttendArgs& a, uint64_t row) {
   const uint32_t lane = threadIdx.x % 32;
   if (row >= (uint64_t)a.n_seqs * a.q_heads) return;
   const uint32_t seq = (uint32_t)(row / a.q_heads), head = (uint32_t)(row - (uint64_t)seq * a.q_heads);
-  uint32_t np = 0;
-  if (a.n_groups) {
-    const uint32_t g = a.group_of(seq);
-    if (g != ~0u) {
-      const Segment p = a.checked(a.prefix, g, a.max_prefix, false);
-      np = (p.tokens + a.chunk_tokens[0] - 1u) / a.chunk_tokens[0];
-    }
-  }
-  const Segment sfx = a.checked(a.suffix, seq, a.max_suffix, false);
-  const uint32_t ns = (sfx.tokens + a.chunk_tokens[1] - 1u) / a.chunk_tokens[1];
+  const Parts parts = parts_of(a, seq);
+  const uint32_t n = parts.np + parts.ns;
   const float* const lse = a.part_lse + row * a.n_parts;
-  auto place = [&](uint32_t i) { return i < np ? i : a.chunks[0] + i - np; };
-  float top = -INFINITY;
-  for (uint32_t i = lane; i < np + ns; i += 32) top = fmaxf(top, lse[place(i)]);
+  const float first = lane < n ? lse[parts.place(lane)] : -INFINITY;
+  float top = first;
+  for (uint32_t i = lane + 32u; i < n; i += 32u) top = fmaxf(top, lse[parts.place(i)]);
 #pragma unroll
   for (int d = 16; d; d /= 2) top = fmaxf(top, __shfl_xor_sync(~0u, top, d));
   const float base = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f;
-  for (uint32_t i = lane; i < np + ns; i += 32) sum += exp2_(lse[place(i)] - base);
+  float sum = exp2_(first - base);
+  for (uint32_t i = lane + 32u; i < n; i += 32u) sum += exp2_(lse[parts.place(i)] - base);
 #pragma unroll
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
-  const float total = sum != 0.0f ? base + log2_(sum) : -INFINITY;
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  // (each lane's elements: two neighbours every 64)
-  for (uint32_t d0 = lane * 2u; d0 < a.dv; d0 += 64u) {
-    float x = 0.0f, y = 0.0f;
-    for (uint32_t i = 0; i < np + ns; ++i) {
-      const float e = lse[place(i)];
-      if (e == -INFINITY) continue;
-      const float c = exp2_(e - base) * inv;
-      const float2 v = *reinterpret_cast<const float2*>(a.part_o + (row * a.n_parts + place(i)) * a.dv + d0);
-      x = __fmaf_rn(c, v.x, x);
-      y = __fmaf_rn(c, v.y, y);
+  if (lane == 0 && a.lse) a.lse[row] = sum != 0.0f ? (base + log2_(sum)) * 0.69314718055994530942f : -INFINITY;
+  T* const out = static_cast<T*>(a.out) + (int64_t)seq * a.out_seq + (int64_t)head * a.out_head;
+  const bool wide = (reinterpret_cast<uintptr_t>(out) & 7u) == 0;
+  for (uint32_t d0 = 0; d0 < a.dv; d0 += 128u) {      // four neighbouring elements a lane
+    const uint32_t d = d0 + lane * 4u;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (uint32_t i0 = 0; i0 < n; i0 += 32u) {
+      const float mine = i0 == 0 ? first : (i0 + lane < n ? lse[parts.place(i0 + lane)] : -INFINITY);
+      const float share = exp2_(mine - base) * inv;
+      const uint32_t most = min(32u, n - i0);
+#pragma unroll 4
+      for (uint32_t i = 0; i < most; ++i) {
+        const float c = __shfl_sync(~0u, share, i);
+        const bool some = __shfl_sync(~0u, mine, i) != -INFINITY;   // (a part of nothing has not been written)
+        if (some && d < a.dv) {
+          const float4 v = *reinterpret_cast<const float4*>(a.part_o + (row * a.n_parts + parts.place(i0 + i)) * a.dv + d);
+          x.x = __fmaf_rn(c, v.x, x.x);
+          x.y = __fmaf_rn(c, v.y, x.y);
+          x.z = __fmaf_rn(c, v.z, x.z);
+          x.w = __fmaf_rn(c, v.w, x.w);
+        }
+      }
     }
-    T* o = static_cast<T*>(a.out) + (int64_t)seq * a.out_seq + (int64_t)head * a.out_head + d0;
-    o[0] = narrow<T>(x);
-    o[1] = narrow<T>(y);
-  }
-  if (lane == 0) {
-    if (a.lse) a.lse[row] = total * 0.69314718055994530942f;
-    if (a.weight) a.part_lse[(uint64_t)a.n_seqs * a.q_heads * a.n_parts + row] = total;   // (what the weights are taken from)
+    if (d >= a.dv) continue;
+    if (wide) {
+      *reinterpret_cast<uint2*>(out + d) = make_uint2(pack2<T>(x.x, x.y), pack2<T>(x.z, x.w));
+    } else {
+      out[d] = narrow<T>(x.x);
+      out[d + 1] = narrow<T>(x.y);
+      out[d + 2] = narrow<T>(x.z);
+      out[d + 3] = narrow<T>(x.w);
+    }
   }
 }
 
-// ---- grains to weights: a group of lanes per (segment, KV head, block) ------------------------------
-
-constexpr int kWeightThreads = 256;
-
-__global__ void __launch_bounds__(kWeightThreads) weight_kernel(const __grid_constant__ AttendArgs a, int kind, uint32_t blocks_most,
-                                                               uint32_t lanes) {
-  wait_for_kernel_ahead();
-  const uint64_t item = ((uint64_t)blockIdx.x * kWeightThreads + threadIdx.x) / lanes;
-  const uint32_t lane = threadIdx.x % lanes;
-  const uint32_t b = (uint32_t)(item % blocks_most);
-  const uint64_t sh = item / blocks_most;
-  const uint32_t head = (uint32_t)(sh % a.tv.heads);
-  const uint64_t index = sh / a.tv.heads;
-  unsigned long long w = 0;
-  uint32_t handle = KV_NONE;
-  if (index < (kind == kKindPrefix ? a.n_groups : a.n_seqs)) {
-    Segment seg;
-    uint32_t seq0 = (uint32_t)index, rows = a.group, stride = a.group;
-    if (kind == kKindPrefix) {
-      uint32_t lo, hi;
-      a.members((uint32_t)index, lo, hi, false);
-      seq0 = lo;
-      rows = (hi - lo) * a.group;
-      stride = a.max_members * a.group;
-      seg = a.checked(a.prefix, (uint32_t)index, a.max_prefix, false);
-    } else {
-      seg = a.checked(a.suffix, (uint32_t)index, a.max_suffix, false);
+// Weight of up to kWeightBlocks blocks of a segment and KV head: the sum over its rows of what the kernels have left for
+// their grains, taken from the rows' own sums.  `lanes` threads a block.
+__device__ __forceinline__ void add_weights(const AttendArgs& a, int kind, uint32_t item, uint32_t lanes, float* total) {
+  const uint32_t most_blocks = ((kind == kKindPrefix ? a.max_prefix : a.max_suffix) + a.tv.block_tokens - 1u) / a.tv.block_tokens;
+  const uint32_t spans = (most_blocks + kWeightBlocks - 1u) / kWeightBlocks;
+  const uint32_t block0 = item % spans * kWeightBlocks;
+  item /= spans;
+  const uint32_t head = item % a.tv.heads, index = item / a.tv.heads;
+  uint32_t seq0 = index, rows = a.group, stride = a.group;
+  Segment seg;
+  if (kind == kKindPrefix) {
+    uint32_t lo, hi;
+    a.members(index, lo, hi, false);
+    seq0 = lo;
+    rows = (hi - lo) * a.group;
+    stride = a.max_members * a.group;
+    seg = a.checked(a.prefix, index, a.max_prefix, false);
+  } else {
+    seg = a.checked(a.suffix, index, a.max_suffix, false);
+  }
+  if (block0 * a.tv.block_tokens >= seg.tokens) return;
+  const uint32_t group = threadIdx.x / lanes, lane = threadIdx.x % lanes, groups = kFinishThreads / lanes;
+  const uint32_t blocks = min(kWeightBlocks, (seg.tokens - 1u) / a.tv.block_tokens + 1u - block0);
+  const float* const grain = a.grain[kind] + ((uint64_t)index * a.tv.heads + head) * a.grains[kind] * stride;
+  for (uint32_t r0 = 0; r0 < rows; r0 += kWeightRows) {
+    const uint32_t here = min(kWeightRows, rows - r0);
+    __syncthreads();
+    for (uint32_t r = threadIdx.x; r < here; r += kFinishThreads) {
+      const uint32_t member = (r0 + r) / a.group, seq = seq0 + member;
+      const uint64_t row = (uint64_t)seq * a.q_heads + head * a.group + (r0 + r - member * a.group);
+      const float* const lse = a.part_lse + row * a.n_parts;
+      if (a.direct) {
+        total[r] = lse[0];
+        continue;
+      }
+      const Parts parts = parts_of(a, seq);
+      float top = -INFINITY, sum = 0.0f;
+      for (uint32_t i = 0; i < parts.np + parts.ns; ++i) top = fmaxf(top, lse[parts.place(i)]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      for (uint32_t i = 0; i < parts.np + parts.ns; ++i) sum += exp2_(lse[parts.place(i)] - base);
+      total[r] = base + log2_(sum);      // (-inf: no parts, or empty ones)
     }
-    const uint32_t from = b * a.tv.block_tokens;
-    if (from < seg.tokens && rows) {
+    __syncthreads();
+    for (uint32_t b0 = 0; b0 < blocks; b0 += groups) {
+      const uint32_t b = block0 + b0 + group;
       const uint64_t at = (uint64_t)seg.row + b;
-      if (a.tv.chunk(at, head) != ~0u) {
+      unsigned long long w = 0;
+      uint32_t handle = KV_NONE;
+      if (b0 + group < blocks && a.tv.chunk(at, head) != ~0u) {
         handle = a.tv.table[(at * a.tv.layers + a.tv.layer) * a.tv.heads + head];
-        const uint32_t to = min(seg.tokens, from + a.tv.block_tokens);
+        const uint32_t from = b * a.tv.block_tokens, to = min(seg.tokens, from + a.tv.block_tokens);
         const uint32_t g0 = from / a.grain_tokens, g1 = (to + a.grain_tokens - 1u) / a.grain_tokens;
-        const float* const total = a.part_lse + (a.direct ? 0ull : (uint64_t)a.n_seqs * a.q_heads * a.n_parts);
-        const float* const grain = a.grain[kind] + (index * a.tv.heads + head) * (uint64_t)a.grains[kind] * stride;
         float sum = 0.0f;
-        for (uint32_t r = lane; r < rows; r += lanes) {
-          const uint32_t member = r / a.group;
-          const float lse = total[(uint64_t)(seq0 + member) * a.q_heads + head * a.group + (r - member * a.group)];
+        for (uint32_t r = lane; r < here; r += lanes) {
+          const float lse = total[r];
           if (lse == -INFINITY) continue;
-          for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r] - lse);
+          for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r0 + r] - lse);
         }
         // in units of 2^-32; NaN counts as nothing
         const float x = sum * 0x1p32f;
         w = x > 0.0f ? __float2ull_rn(fminf(x, 0x1p62f)) : 0ull;
       }
+      for (uint32_t d = lanes / 2u; d; d /= 2u) w += __shfl_xor_sync(~0u, w, d);
+      if (lane == 0 && w) atomicAdd(a.weight + handle, w);
     }
   }
-  for (uint32_t d = lanes / 2u; d; d /= 2u) w += __shfl_xor_sync(~0u, w, d);
-  if (lane == 0 && w) atomicAdd(a.weight + handle, w);
+}
+
+// CTAs: rows to join, then spans of prefixes, then spans of suffixes.
+template <typename T>
+__global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ AttendArgs a, uint32_t join_ctas, uint32_t prefix_ctas,
+                                                                uint32_t prefix_lanes, uint32_t suffix_lanes) {
+  __shared__ float total[kWeightRows];
+  wait_for_kernel_ahead();
+  const uint32_t i = blockIdx.x;
+  if (i < join_ctas) join_rows<T>(a, (uint64_t)i * kFinishRows + threadIdx.x / 32);
+  else if (i < join_ctas + prefix_ctas) add_weights(a, kKindPrefix, i - join_ctas, prefix_lanes, total);
+  else add_weights(a, kKindSuffix, i - join_ctas - prefix_ctas, suffix_lanes, total);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
@@ -677,9 +656,21 @@ cudaError_t launch_rows_by(const AttendArgs& a, uint32_t rows, bool prefix, bool
 template <typename T>
 cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  const bool prefix = a.chunks[0] > 0, tp = prefix && a.tiles[0], ts = a.tiles[1], rp = prefix && !tp, rs = !ts;
+  const bool prefix = a.chunks[0] > 0, tp = prefix && a.tiles[0], ts = a.tiles[1];
+  const bool sp = prefix && a.stream[0], ss = a.stream[1], rp = prefix && !tp && !sp, rs = !ts && !ss;
   if (tp || ts) e = launch_attend_tiles(a, dtype, mla, tp, ts, s);
   if (e != cudaSuccess) return e;
+  if (sp || ss) {
+    const uint32_t rows = a.max_members * a.group;
+    const bool behind = tp || ts;
+    if (sp && ss && (rows <= 16) != (a.group <= 16)) {
+      e = launch_attend_stream(a, dtype, rows, true, false, behind, s);
+      if (e == cudaSuccess) e = launch_attend_stream(a, dtype, a.group, false, true, false, s);
+    } else {
+      e = launch_attend_stream(a, dtype, ss ? a.group : rows, sp, ss, behind, s);
+    }
+    if (e != cudaSuccess) return e;
+  }
   if (mla) {
     using L = Latent<T, 4, 2>;
     if (rp || rs) e = launch_items(latent_kernel<T, 4, 2>, 4 * 2 * 32, L::kSmem, a, L::kRows, L::kRows, rp, rs, s);
@@ -699,23 +690,22 @@ cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t 
   }
   if (e != cudaSuccess) return e;
   const uint64_t rows = (uint64_t)a.n_seqs * a.q_heads;
-  if (!a.direct)
-    e = launch_overlapped(join_kernel<T>, (unsigned)((rows + kJoinThreads / 32 - 1) / (kJoinThreads / 32)), (unsigned)kJoinThreads, s, a);
-  if (e != cudaSuccess || !a.weight) return e;
-  for (int kind = prefix ? 0 : 1; kind < 2; ++kind) {
-    const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
-    const uint32_t blocks = (most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
-    if (!blocks) continue;
-    const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
-    uint32_t lanes = 1;
-    while (lanes < 32u && lanes < r) lanes *= 2u;
-    const uint64_t items = (uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks;
-    const uint64_t grid = (items * lanes + kWeightThreads - 1) / kWeightThreads;
-    if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
-    e = launch_overlapped(weight_kernel, (unsigned)grid, (unsigned)kWeightThreads, s, a, kind, blocks, lanes);
-    if (e != cudaSuccess) return e;
+  const uint64_t join = a.direct ? 0 : (rows + kFinishRows - 1) / kFinishRows;
+  uint64_t spans[2] = {0, 0};
+  uint32_t lanes[2] = {1, 1};
+  if (a.weight) {
+    for (int kind = prefix ? 0 : 1; kind < 2; ++kind) {
+      const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
+      const uint64_t blocks = ((uint64_t)most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
+      spans[kind] = (uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * ((blocks + kWeightBlocks - 1) / kWeightBlocks);
+      const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
+      while (lanes[kind] < 32u && lanes[kind] < r) lanes[kind] *= 2u;
+    }
   }
-  return e;
+  const uint64_t grid = join + spans[0] + spans[1];
+  if (!grid) return cudaSuccess;
+  if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
+  return launch_overlapped(finish_kernel<T>, (unsigned)grid, (unsigned)kFinishThreads, s, a, (uint32_t)join, (uint32_t)spans[0], lanes[0], lanes[1]);
 }
 
 }  // namespace

@@ -131,4 +131,87 @@ __device__ __forceinline__ float* grain_at(const AttendArgs& a, const Item& w, u
   return a.grain[w.kind] + (((uint64_t)w.index * a.tv.heads + w.head) * a.grains[w.kind] + gr) * rows + w.row0;
 }
 
+// ---- products of 16 rows on mma.sync ----
+
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <>
+__device__ __forceinline__ void mma<__nv_bfloat16>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <>
+__device__ __forceinline__ void mma<__half>(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+  return fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+}
+__device__ __forceinline__ float quad_sum(float x) {
+  x += __shfl_xor_sync(~0u, x, 1);
+  return x + __shfl_xor_sync(~0u, x, 2);
+}
+
+// kN warps that have worked on different tokens for the same 16 kM rows join: maxima and sums, then outputs.  All threads of
+// the CTA; memory: kN * 16 kM * (D + 2) floats, which nobody uses any more.
+template <int D, int kM, int kN>
+__device__ __forceinline__ void join_warps(uint8_t* memory, int wm, int wn, const float (&o)[D / 8][4], const float (&m)[2], const float (&l)[2]) {
+  float* const o_s = reinterpret_cast<float*>(memory);                        // [kN][16 kM][D]
+  float* const ml_s = o_s + kN * kM * 16 * D;                                 // [kN][16 kM][2]
+  const int lane = threadIdx.x % 32;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = wm * 16 + lane / 4 + h * 8;
+    if ((lane & 3) == 0) {
+      ml_s[(wn * kM * 16 + r) * 2] = m[h];
+      ml_s[(wn * kM * 16 + r) * 2 + 1] = l[h];
+    }
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j)
+      *reinterpret_cast<float2*>(o_s + (wn * kM * 16 + r) * D + ((j ^ (r & 7)) * 8 + (lane & 3) * 2)) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
+  }
+}
+template <typename T, int D, int kM, int kN>
+__device__ __forceinline__ void put_joined(const AttendArgs& a, const Item& w, uint32_t part, const uint8_t* memory) {
+  const float* const o_s = reinterpret_cast<const float*>(memory);
+  const float* const ml_s = o_s + kN * kM * 16 * D;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < w.rows * (D / 2); i += blockDim.x) {
+    const uint32_t r = i / (D / 2), d = i % (D / 2) * 2u;
+    if (d >= a.dv) continue;
+    float top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) top = fmaxf(top, ml_s[(n * kM * 16 + r) * 2]);
+    const float from = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+    for (int n = 0; n < kN; ++n) {
+      const float c = exp2_(ml_s[(n * kM * 16 + r) * 2] - from);
+      const float2 v = *reinterpret_cast<const float2*>(o_s + (n * kM * 16 + r) * D + (((d / 8u) ^ (r & 7u)) * 8u + d % 8u));
+      sum += c * ml_s[(n * kM * 16 + r) * 2 + 1];
+      x += c * v.x;
+      y += c * v.y;
+    }
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+    uint32_t seq, head;
+    row_of(a, w, r, seq, head);
+    put2<T>(a, seq, head, part, d, x * inv, y * inv);
+    if (d == 0) put_lse(a, seq, head, part, sum != 0.0f ? top + log2_(sum) : -INFINITY);
+  }
+}
+
 }  // namespace kvt

@@ -1,0 +1,315 @@
+// kv_attend where few rows read a block: a stream of blocks through independent warps (and the encoder of the maps
+// by which the kernels here and in kv_attend_tiles.cu copy blocks).
+//
+// A CTA's chunk of a segment is dealt out to its warps in units of 16 tokens of one block; a block that is not in HBM is no
+// unit.  Each warp has a ring of units of its own, filled by TMA (a box of 16 rows x 64 elements, swizzled, for each
+// panel of K and V) which the warp itself issues as it empties them: no barrier between warps until they join at the end.
+// A unit's scores (16 kM rows x 16 tokens) and output are mma.sync products whose operands come from the ring by ldmatrix,
+// free of bank conflicts thanks to the swizzle.  The output is rescaled only when a maximum has grown by more than 2^8.
+// Bound: HBM.  Four warps with three units of 8 KB each, two CTAs an SM, keep 128 KB or more in flight on every SM.
+#include "kv_attend_device.cuh"
+#include "kv_attend_tma.cuh"
+
+namespace kvt {
+namespace {
+
+constexpr int kUnit = 16;        // tokens
+constexpr int kStreamWarps = 4;
+constexpr uint32_t kMaxUnits = kMaxChunkTokens / kUnit;
+
+template <int D, int kM>
+struct Stream {
+  static constexpr int kPanels = D / 64, kPanelBytes = kUnit * 128, kUnitBytes = 2 * kPanels * kPanelBytes;
+  static constexpr int kSlots = D == 128 ? 3 : 6;
+  static constexpr size_t kRing = (size_t)kStreamWarps * kSlots * kUnitBytes;
+  static constexpr size_t kJoin = (size_t)kStreamWarps * kM * 16 * (D + 2) * 4;
+  static constexpr size_t kUnits = (kRing > kJoin ? kRing : kJoin);      // what follows the ring: the list of units, barriers
+  static constexpr size_t kSmem = 1024 + kUnits + kMaxUnits * 8 + kStreamWarps * kSlots * 8 + 16;
+};
+
+template <typename T, int D, int kM>
+__global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
+                                                                   uint32_t first_kind_items, uint32_t behind_tiles) {
+  using S = Stream<D, kM>;
+  extern __shared__ uint8_t raw[];
+  uint8_t* const smem = raw + ((1024u - (smem_address(raw) & 1023u)) & 1023u);
+  uint2* const units = reinterpret_cast<uint2*>(smem + S::kUnits);                     // (first row in the slab, first token)
+  unsigned long long* const bars = reinterpret_cast<unsigned long long*>(units + kMaxUnits);
+  uint32_t* const control = reinterpret_cast<uint32_t*>(bars + kStreamWarps * S::kSlots);   // units, gave up
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  // Behind a launch of the tiles kernel, which has waited for all that is ahead of it, the two may run side by side; this
+  // one then ends only when that one has.
+  if (behind_tiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  else wait_for_kernel_ahead();
+  struct AtEnd {
+    uint32_t wait;
+    __device__ ~AtEnd() {
+      if (wait) asm volatile("griddepcontrol.wait;" ::: "memory");
+    }
+  } at_end{behind_tiles};
+
+  Item w;
+  const bool second = blockIdx.x >= first_kind_items;
+  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? blockIdx.x - first_kind_items : blockIdx.x, kM * 16, w, threadIdx.x == 0)) return;
+  if (w.to == 0) {
+    put_nothing<T>(a, w);
+    return;
+  }
+  const TableView& tv = a.tv;
+  if (warp == 0) {
+    const uint32_t n = (w.to - w.from + kUnit - 1u) / kUnit;
+    uint32_t found = 0;
+    for (uint32_t u0 = 0; u0 < n; u0 += 128u) {
+      uint32_t ch[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t u = u0 + k * 32u + lane;
+        ch[k] = u < n ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(w.from + u * kUnit), w.head) : ~0u;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t at = w.from + (u0 + k * 32u + lane) * kUnit;
+        const uint32_t there = __ballot_sync(~0u, ch[k] != ~0u);
+        if (ch[k] != ~0u)
+          units[found + __popc(there & ((1u << lane) - 1u))] = make_uint2(ch[k] * tv.block_tokens + (at - tv.by_tokens(at) * tv.block_tokens), at);
+        found += __popc(there);
+      }
+    }
+    if (lane == 0) {
+      control[0] = found;
+      control[1] = 0;
+    }
+  } else if (threadIdx.x == 32) {
+    for (int b = 0; b < kStreamWarps * S::kSlots; ++b) bar_init(smem_address(bars + b), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  // queries straight into the operands' registers: rows lane / 4 and 8 further on, elements 2 (lane % 4) and 8 further on
+  uint32_t q[kM][D / 16][4];
+#pragma unroll
+  for (int i = 0; i < kM; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t r = i * 16 + lane / 4 + h * 8;
+      const bool there = r < w.rows;
+      uint32_t seq = 0, head = 0;
+      if (there) row_of(a, w, r, seq, head);
+      const uint16_t* const src = static_cast<const uint16_t*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + (lane & 3) * 2;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) q[i][k][h + 2 * e] = there ? (uint32_t)src[k * 16 + e * 8] | (uint32_t)src[k * 16 + e * 8 + 1] << 16 : 0u;
+    }
+  __syncthreads();
+  const uint32_t n_units = control[0];
+  volatile uint32_t* const gave_up = control + 1;
+  uint8_t* const ring = smem + warp * (S::kSlots * S::kUnitBytes);
+  unsigned long long* const bar = bars + warp * S::kSlots;
+  auto issue = [&](uint32_t j, uint32_t slot) {      // unit j into a slot, by the first lane
+    if (lane == 0 && j < n_units) {
+      const uint32_t dst = smem_address(ring + slot * S::kUnitBytes), b = smem_address(bar + slot);
+      const int32_t y = (int32_t)units[j].x;
+      bar_expect(b, S::kUnitBytes);
+#pragma unroll
+      for (int p = 0; p < S::kPanels; ++p) {
+        tma_box(dst + p * S::kPanelBytes, &map, p * 64, y, b);
+        tma_box(dst + (S::kPanels + p) * S::kPanelBytes, &map, p * 64, y + (int32_t)(tv.heads * tv.block_tokens), b);
+      }
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < S::kSlots; ++k) issue(warp + k * kStreamWarps, k);
+
+  float o[kM][D / 8][4], m[kM][2], l[kM][2];
+#pragma unroll
+  for (int i = 0; i < kM; ++i) {
+    m[i][0] = m[i][1] = -INFINITY;
+    l[i][0] = l[i][1] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
+  }
+  const uint32_t k_row = (lane >> 4) * 8 + (lane & 7), v_row = (lane >> 3 & 1) * 8 + (lane & 7);
+  uint32_t slot = 0, parity = 0;
+  for (uint32_t j = warp; j < n_units; j += kStreamWarps) {
+    if (!__all_sync(~0u, bar_wait(smem_address(bar + slot), parity, gave_up, tv.status))) break;
+    uint8_t* const unit = ring + slot * S::kUnitBytes;
+    const uint32_t k_at = smem_address(unit) + k_row * 128, v_at = smem_address(unit) + S::kPanels * S::kPanelBytes + v_row * 128;
+    const uint32_t at = units[j].y, left = w.to - at;
+    if (left < (uint32_t)kUnit) {
+      // what lies behind the last token would meet probabilities of zero: it may be anything
+      for (uint32_t x = lane; x < (kUnit - left) * S::kPanels * 8u; x += 32u) {
+        const uint32_t tok = left + x / (S::kPanels * 8u), c = x % (S::kPanels * 8u);
+        *reinterpret_cast<uint4*>(unit + (S::kPanels + c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+      }
+      __syncwarp();
+    }
+    // scores, the even and the odd steps of the sum on their own
+    float s[kM][2][2][4];
+#pragma unroll
+    for (int i = 0; i < kM; ++i)
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[i][x / 8][x / 4 % 2][x % 4] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      uint32_t b[4];
+      const uint32_t c = 2 * k + (lane >> 3 & 1);
+      ldmatrix4(b, k_at + c / 8 * S::kPanelBytes + (((c & 7) ^ (k_row & 7)) * 16));
+#pragma unroll
+      for (int i = 0; i < kM; ++i) {
+        mma<T>(s[i][k & 1][0], q[i][k], b[0], b[1]);
+        mma<T>(s[i][k & 1][1], q[i][k], b[2], b[3]);
+      }
+    }
+    uint32_t p[kM][4];
+#pragma unroll
+    for (int i = 0; i < kM; ++i) {
+      float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = (s[i][0][n][e] + s[i][1][n][e]) * a.scale2;
+          if (left < (uint32_t)kUnit && n * 8u + (lane & 3) * 2u + (e & 1) >= left) x = -INFINITY;
+          s[i][0][n][e] = x;
+          top[e >> 1] = fmaxf(top[e >> 1], x);
+        }
+      // the base follows the maximum when it has grown by 8 (or from nothing)
+      float turn[2] = {1.0f, 1.0f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float mx = quad_max(top[h]);
+        if (mx > m[i][h] + 8.0f || (m[i][h] == -INFINITY && mx > m[i][h])) {
+          turn[h] = exp2_(m[i][h] - mx);
+          m[i][h] = mx;
+          l[i][h] *= turn[h];
+        }
+      }
+      if (__any_sync(~0u, turn[0] != 1.0f || turn[1] != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < D / 8; ++d) {
+          o[i][d][0] *= turn[0];
+          o[i][d][1] *= turn[0];
+          o[i][d][2] *= turn[1];
+          o[i][d][3] *= turn[1];
+        }
+      }
+      const float base[2] = {m[i][0] == -INFINITY ? 0.0f : m[i][0], m[i][1] == -INFINITY ? 0.0f : m[i][1]};
+      float part[2] = {0.0f, 0.0f};
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = exp2_(s[i][0][n][e] - base[e >> 1]);
+          s[i][0][n][e] = x;
+          part[e >> 1] += x;
+        }
+        p[i][2 * n] = pack2<T>(s[i][0][n][0], s[i][0][n][1]);
+        p[i][2 * n + 1] = pack2<T>(s[i][0][n][2], s[i][0][n][3]);
+      }
+      l[i][0] += part[0];
+      l[i][1] += part[1];
+      if (a.weight) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float sum = quad_sum(part[h]);
+          const uint32_t r = i * 16 + lane / 4 + h * 8;
+          if ((lane & 3) == 0 && r < w.rows) grain_at(a, w, at / 16u)[r] = base[h] + log2_(sum);
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) {
+      uint32_t b[4];
+      const uint32_t c = 2 * d + (lane >> 4);
+      ldmatrix4t(b, v_at + c / 8 * S::kPanelBytes + (((c & 7) ^ (v_row & 7)) * 16));
+#pragma unroll
+      for (int i = 0; i < kM; ++i) {
+        mma<T>(o[i][2 * d], p[i], b[0], b[1]);
+        mma<T>(o[i][2 * d + 1], p[i], b[2], b[3]);
+      }
+    }
+    __syncwarp();
+    issue(j + S::kSlots * kStreamWarps, slot);
+    if (++slot == S::kSlots) {
+      slot = 0;
+      parity ^= 1u;
+    }
+  }
+  if (*gave_up) {
+    // copies in flight end before the memory is given back
+    for (uint32_t k = 0; k < 1u << 16; ++k) asm volatile("nanosleep.u32 1000;");
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kM; ++i) {
+    l[i][0] = quad_sum(l[i][0]);
+    l[i][1] = quad_sum(l[i][1]);
+    join_warps<D, kM, kStreamWarps>(smem, i, warp, o[i], m[i], l[i]);
+  }
+  put_joined<T, D, kM, kStreamWarps>(a, w, part_of(a, w), smem);
+}
+
+typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                           const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// The driver's encoder (its address does not change while the process runs).
+Encode encoder() {
+  static const Encode f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<Encode>(p);
+  }();
+  return f;
+}
+
+template <typename T, int D, int kM>
+cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
+  using S = Stream<D, kM>;
+  const TableView& tv = a.tv;
+  CUtensorMap map;
+  if (!block_map(tv, D, kUnit, &map)) return cudaErrorInvalidValue;
+  const uint64_t rows = (uint64_t)a.max_members * a.group, tile = kM * 16;
+  const uint64_t np = prefix ? (rows + tile - 1) / tile * a.chunks[0] * tv.heads * a.n_groups : 0;
+  const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
+  if (np + ns == 0) return cudaSuccess;
+  if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
+  auto* kernel = stream_kernel<T, D, kM>;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
+  if (e != cudaSuccess) return e;
+  return launch_overlapped_smem(kernel, (unsigned)(np + ns), (unsigned)kStreamWarps * 32, S::kSmem, s, a, map, (uint32_t)np, behind_tiles ? 1u : 0u);
+}
+
+template <typename T>
+cudaError_t launch_typed(const AttendArgs& a, uint32_t rows, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
+  if (a.dk == 128) return rows <= 16 ? launch<T, 128, 1>(a, prefix, suffix, behind_tiles, s) : launch<T, 128, 2>(a, prefix, suffix, behind_tiles, s);
+  return rows <= 16 ? launch<T, 64, 1>(a, prefix, suffix, behind_tiles, s) : launch<T, 64, 2>(a, prefix, suffix, behind_tiles, s);
+}
+
+}  // namespace
+
+bool has_block_map() { return encoder() != nullptr; }
+
+bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, CUtensorMap* map) {
+  const Encode f = encoder();
+  const cuuint64_t dims[2] = {dk, tv.n * tv.n_chunks * tv.block_tokens}, strides[1] = {(cuuint64_t)dk * 2};
+  const cuuint32_t box[2] = {64, box_rows}, steps[2] = {1, 1};
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, tv.slab, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows) {
+  return !mla && (dk == 128 || dk == 64) && block_tokens % kUnit == 0 && slab_rows < 0x7fff0000ull && has_block_map();
+}
+
+cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, uint32_t rows, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
+  return dtype == KV_DTYPE_BF16 ? launch_typed<__nv_bfloat16>(a, rows, prefix, suffix, behind_tiles, s)
+                                : launch_typed<__half>(a, rows, prefix, suffix, behind_tiles, s);
+}
+
+}  // namespace kvt

@@ -20,54 +20,12 @@
 //
 // Every wait is bounded: one that gives up sets KV_DEV_WAIT_EXPIRED and a flag that ends the other
 // waits; copies and matrix instructions in flight are then waited for (bounded) before the CTA leaves.
-#include <cuda.h>
-
 #include "kv_attend_device.cuh"
+#include "kv_attend_tma.cuh"
 
 namespace kvt {
 namespace {
 
-constexpr long long kWaitLimit = 4'000'000'000ll;   // cycles of the SM: about two seconds
-
-__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(done)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return done != 0;
-}
-// False: this wait, or another of the CTA, has given up.
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up, uint32_t* status) {
-  if (bar_try(bar, parity)) return true;
-  const long long from = clock64();
-  do {
-    if (bar_try(bar, parity)) return true;
-    if (*gave_up) return false;
-  } while (clock64() - from < kWaitLimit);
-  *gave_up = 1u;
-  atomicOr(status, KV_DEV_WAIT_EXPIRED);
-  return false;
-}
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void commit(uint32_t bar) {
@@ -167,7 +125,7 @@ struct Shape {
   static constexpr int kAPanels = kLatent ? (kDk - kCols) / 64 : kDk / 64, kBPanels = kCols / 64;
   static constexpr int kKBytes = kAPanels * kPanelBytes, kVBytes = kBPanels * kPanelBytes;
   static constexpr int kQBytes = kTiles * kQPanels * 128 * 128;
-  static constexpr int kMasks = kStages + 2;
+  static constexpr int kMasks = kStages + 2;                // a mask is written again kStages + 2 tiles on, see the softmax
   static constexpr int kFirst = kTiles == 2 ? 4 : 2;        // first warp of the softmax
   static constexpr int kThreads = (kFirst + 4 * kTiles) * 32;
   // tensor memory columns: outputs, then scores, then Q
@@ -175,6 +133,7 @@ struct Shape {
   static constexpr int kSAt = kTiles * kCols, kQAt = kSAt + kSlots * kTok;
   static constexpr int kTmem = 512;
   static_assert(kQAt + kQTmem / 2 <= kTmem, "tensor memory");
+  static_assert(kTok == 64, "four grains of weight");
   static constexpr int kControl = 1024;
   static constexpr size_t kSmem = (size_t)kQBytes + kStages * (kKBytes + kVBytes) + kControl + 1024;
 };
@@ -321,7 +280,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w,
   fence_before();
 }
 
-template <typename T, typename S>
+template <typename T, typename S, bool kWeights>
 __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
                                                                uint32_t first_kind_items, uint32_t box_rows, uint32_t outside,
                                                                uint32_t q_sign, uint32_t q_bits) {
@@ -413,7 +372,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         if (!ok) break;
         const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
         if (lane == 0) {
-          if (part == 1) {   // (the softmax reads it behind v_full, and v_empty says that it has)
+          if (part == 0) {   // (ahead of the copies that the scores wait for)
 #pragma unroll
             for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
           }
@@ -451,9 +410,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       for (uint32_t t = 0; t < n_tiles; ++t) {
         const int slot = 2 * r + (int)(t & 1);
         const uint32_t s_at = tmem + (lane_at << 16) + S::kSAt + slot * S::kTok;
-        // (the tile's mask was written ahead of the copies of its second part)
-        ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status) &&
-             bar_wait(smem_address(&ctl->s_full[slot]), (t >> 1) & 1, gave_up, status);
+        // (the tile's mask was written ahead of the copies that the scores have waited for, and is not written
+        // again before scores that wait for this tile's output are complete)
+        ok = bar_wait(smem_address(&ctl->s_full[slot]), (t >> 1) & 1, gave_up, status);
         ok = __all_sync(~0u, ok);
         if (!ok) break;
         fence_after();
@@ -512,22 +471,21 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
           tmem_wait_store();
         }
 #pragma unroll
-        for (int g = 0; g < S::kTok / 16; ++g) {
-          Pair sum(0.0f, 0.0f);
+        for (int e = 0; e < S::kTok; e += 2) fma2(Pair(s[e], s[e + 1]), scale, minus).get(s[e], s[e + 1]);
+        Pair sums[4] = {Pair(0.0f, 0.0f), Pair(0.0f, 0.0f), Pair(0.0f, 0.0f), Pair(0.0f, 0.0f)};
 #pragma unroll
-          for (int e = g * 16; e < g * 16 + 16; e += 2) {
-            float x, y;
-            fma2(Pair(s[e], s[e + 1]), scale, minus).get(x, y);
-            x = exp2_(x);
-            y = exp2_(y);
-            sum = add2(sum, Pair(x, y));
-            bits[e / 2] = pack2<T>(x, y);
-          }
+        for (int e = 0; e < S::kTok; e += 2) {
+          const float x = exp2_(s[e]), y = exp2_(s[e + 1]);
+          sums[kWeights ? e / 16 : e / 2 % 4] = add2(sums[kWeights ? e / 16 : e / 2 % 4], Pair(x, y));   // (with weights: by grains)
+          bits[e / 2] = pack2<T>(x, y);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
           float lo, hi;
-          sum.get(lo, hi);
+          sums[g].get(lo, hi);
           const float both = lo + hi;
           l += both;
-          if (a.weight && mine && col0 == 0 && w.from + t * S::kTok + g * 16u < w.to)
+          if (kWeights && mine && col0 == 0 && w.from + t * S::kTok + g * 16u < w.to)
             grain_at(a, w, (w.from + t * S::kTok) / 16u + g)[row] = base + log2_(both);
         }
 #pragma unroll
@@ -536,6 +494,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         // what lies behind the last token, in its block, would meet probabilities of zero: it may be anything
         const uint32_t left = w.to - (w.from + t * S::kTok);
         if (left < (uint32_t)S::kTok && left % box_rows) {
+          ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
           uint8_t* const vt = ring + (t % S::kStages) * (S::kKBytes + S::kVBytes) + S::kKBytes;
           const uint32_t end = (left + box_rows - 1u) / box_rows * box_rows;
           for (uint32_t x = lane_at + lane; x < (end - left) * (S::kCols / 8u); x += 128u) {
@@ -594,41 +555,20 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   }
 }
 
-typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                           const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-// The driver's encoder (its address does not change while the process runs).
-Encode encoder() {
-  static const Encode f = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult r;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
-      (void)cudaGetLastError();
-      p = nullptr;
-    }
-    return reinterpret_cast<Encode>(p);
-  }();
-  return f;
-}
-
 template <typename T, typename S>
 cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s) {
   const TableView& tv = a.tv;
   const uint32_t box = tv.block_tokens < (uint32_t)S::kTok ? tv.block_tokens : (uint32_t)S::kTok;
   const uint64_t rows = tv.n * tv.n_chunks * tv.block_tokens;
   CUtensorMap map;
-  const cuuint64_t dims[2] = {(cuuint64_t)S::kDk, rows}, strides[1] = {(cuuint64_t)S::kDk * 2};
-  const cuuint32_t box_dims[2] = {64, box}, steps[2] = {1, 1};
-  if (encoder()(&map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, tv.slab, dims, strides, box_dims, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-    return cudaErrorInvalidValue;
+  if (!block_map(tv, S::kDk, box, &map)) return cudaErrorInvalidValue;
   const uint64_t tile = S::kTiles * 128;
   const uint64_t np = prefix ? ((uint64_t)a.max_members * a.group + tile - 1) / tile * a.chunks[0] * tv.heads * a.n_groups : 0;
   const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   const uint64_t grid = (np + ns) * (S::kDv / S::kCols);
   if (grid == 0) return cudaSuccess;
   if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
-  auto* kernel = tiles_kernel<T, S>;
+  auto* kernel = a.weight ? tiles_kernel<T, S, true> : tiles_kernel<T, S, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
   AttendArgs b = a;
@@ -663,7 +603,7 @@ bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint6
   if (block_tokens % 8 != 0 || (tok % block_tokens != 0 && block_tokens % tok != 0)) return false;
   if (weights && block_tokens % 16 != 0) return false;   // (they are kept by 16 tokens)
   // (a box's place is a signed number of rows)
-  return slab_rows < 0x7fff0000ull && encoder() != nullptr;
+  return slab_rows < 0x7fff0000ull && has_block_map();
 }
 
 cudaError_t launch_attend_tiles(const AttendArgs& a, int dtype, bool mla, bool prefix, bool suffix, cudaStream_t s) {

@@ -47,9 +47,9 @@ TableView table_view(const PoolView& v, int32_t q, int32_t layer, const uint32_t
 // How a call's work is split: tokens of a chunk and chunks, for prefixes and suffixes.
 constexpr uint32_t kSms = 148;
 // Rows from which on a segment goes to the tensor cores' 128-row tiles.
-constexpr uint32_t kTileRows = 48;
+constexpr uint32_t kTileRows = 33;
 struct Split {
-  bool tiles[2];
+  bool tiles[2], stream[2];
   uint32_t chunk_tokens[2], chunks[2], n_parts, grain_tokens, grains[2];
   uint64_t lse_at, grain_at[2], bytes;
 };
@@ -87,16 +87,19 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
   if (max_suffix >= 0x40000000u || max_prefix >= 0x40000000u || n_seqs >= 0x1000000u || n_groups >= 0x1000000u) return false;
   if (max_members > n_seqs) max_members = n_seqs;
   if ((uint64_t)max_members * group >= 0x10000000u || (uint64_t)n_seqs * q_heads >= 0x40000000u) return false;
-  out->tiles[0] = out->tiles[1] = false;
+  out->tiles[0] = out->tiles[1] = out->stream[0] = out->stream[1] = false;
   out->chunk_tokens[0] = out->chunk_tokens[1] = 64;
   out->chunks[0] = out->chunks[1] = 0;
   const uint64_t prefix_rows = (uint64_t)max_members * group;
-  const bool fits = tiles_take(dk, dv, mla, bt, v.geom[q].n * v.geom[q].n_chunks * bt, weights);
+  const uint64_t slab_rows = v.geom[q].n * v.geom[q].n_chunks * bt;
+  const bool streams = stream_takes(dk, dv, mla, bt, slab_rows);
+  const bool fits = tiles_take(dk, dv, mla, bt, slab_rows, weights);
   for (int k = 0; k < 2; ++k) {
     if (k == 0 && !shared) continue;
     const uint64_t rows = k == 0 ? prefix_rows : group, segs = (uint64_t)(k == 0 ? n_groups : n_seqs) * heads;
     const uint32_t most = k == 0 ? max_prefix : max_suffix ? max_suffix : 1;
     out->tiles[k] = fits && rows >= kTileRows;
+    out->stream[k] = !out->tiles[k] && streams && rows <= 32;
     if (out->tiles[k]) {
       const uint64_t tile = mla ? 128 : 256;
       split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, bt, &out->chunk_tokens[k], &out->chunks[k]);
@@ -111,7 +114,7 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
   unsigned __int128 at = 0;
   auto take = [&at](unsigned __int128 bytes) { const uint64_t o = (uint64_t)at; at = (at + bytes + 255) / 256 * 256; return o; };
   if (out->n_parts > 1) take(rows * out->n_parts * dv * 4);
-  out->lse_at = take(rows * (out->n_parts + 1) * 4);
+  out->lse_at = take(rows * out->n_parts * 4);
   for (int k = 0; k < 2; ++k) {
     const uint32_t most = k == 0 ? (shared ? max_prefix : 0) : max_suffix;
     out->grains[k] = (uint32_t)(((uint64_t)most + out->grain_tokens - 1) / out->grain_tokens);
@@ -189,6 +192,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   uint8_t* const scratch = static_cast<uint8_t*>(d->d_scratch);
   for (int k = 0; k < 2; ++k) {
     a.tiles[k] = sp.tiles[k];
+    a.stream[k] = sp.stream[k];
     a.chunk_tokens[k] = sp.chunk_tokens[k];
     a.chunks[k] = sp.chunks[k];
     a.grains[k] = sp.grains[k];

@@ -207,6 +207,8 @@ def _pool(s):
             _ok(pool.kv_demote(torch.arange(s["resident"], s["n"], dtype=torch.int32, device="cuda"), s["n"] - s["resident"], 1 << 19))
             pool.sync()
         pool.tag[: s["resident"]] = s["tag"][: s["resident"]]
+        pool.loc.fill_(NONE)            # (handles of other entries are nowhere)
+        pool.loc[s["tag"][: s["resident"]].long()] = torch.arange(s["resident"], dtype=torch.int32, device="cuda")
         pool.last_epoch[: s["n"]] = s["last_epoch"]
         s["victims"] = torch.empty(max(4, s["k"]), dtype=torch.int32, device="cuda")
     else:

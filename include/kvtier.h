@@ -571,15 +571,16 @@ int32_t kv_attend(kv_pool* pool, const kv_attend_desc* desc, kv_stream_t stream)
 uint64_t kv_attend_scratch_bytes(kv_pool* pool, int32_t partition, uint32_t n_seqs, uint32_t n_groups,
                                  uint32_t max_suffix, uint32_t max_prefix, uint32_t max_members, int32_t weights);
 
-/* kv_attention_score: eviction by accumulated attention weight.  For every RESIDENT entry, g its
- * handle (binary32, each operation rounded once):
+/* kv_attention_score: eviction by accumulated attention weight.  For every RESIDENT entry, g the
+ * handle that the pool gave it (d_tag; d_loc[g] is the entry), in binary32, each operation rounded once:
  *   d_acc[g] = decay * d_acc[g] + float(d_weight[g]) * 2^-32,  d_weight[g] = 0,
  *   d_score[entry] = d_acc[g], or +inf if fewer than `protect` epochs lie between the entry's last
  *                    epoch (its last touch, or its admission) and `epoch`;
  * FREE entries get +inf.  kv_select_victims (or kv_select_victim_blocks) then chooses the lowest.
  * d_weight (device, u64 [n_tags]) and d_acc (device, f32 [n_tags]) are zeroed by the caller once; they
  * belong to handles, so a block keeps what it has gathered while it is in the host tier, where it does not decay.
- * 0 <= decay <= 1; protect < 2^31.  The pool's predictor, EMA and touches are left alone. */
+ * Handles are gone through by d_loc; a caller that has led a second handle to an entry gets the score of either.
+ * 0 <= decay <= 1; protect < 2^31, 0: no entry is young.  The pool's predictor, EMA and touches are left alone. */
 int32_t kv_attention_score(kv_pool* pool, uint32_t epoch, float decay, uint32_t protect, uint64_t* d_weight,
                            float* d_acc, kv_stream_t stream);
 

@@ -152,8 +152,7 @@ struct AppendArgs {
 cudaError_t launch_append(const AppendArgs& a, int dtype, bool wide, cudaStream_t s);
 
 // kv_attention.cu
-cudaError_t launch_attention_score(const EntryState& st, uint32_t epoch, float decay, uint32_t protect,
-                                   unsigned long long* weight, float* acc, uint64_t n_tags, uint32_t* status,
-                                   cudaStream_t s);
+cudaError_t launch_attention_score(const EntryState& st, const uint32_t* loc, uint64_t n_tags, uint32_t epoch, float decay, uint32_t protect,
+                                   unsigned long long* weight, float* acc, cudaStream_t s);
 
 }  // namespace kvt

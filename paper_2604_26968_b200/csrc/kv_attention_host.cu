@@ -271,8 +271,8 @@ int32_t kv_attention_score(kv_pool* p, uint32_t epoch, float decay, uint32_t pro
   const int32_t rs = pool_settle(p, stream);
   if (rs != KV_OK) return rs;
   const PoolView v = pool_view(p);
-  return pool_cuda_error(p, launch_attention_score(v.st, epoch, decay, protect, reinterpret_cast<unsigned long long*>(d_weight), d_acc,
-                                                   v.desc->n_tags, v.status, S(stream)));
+  return pool_cuda_error(p, launch_attention_score(v.st, v.desc->d_loc, v.desc->n_tags, epoch, decay, protect,
+                                                   reinterpret_cast<unsigned long long*>(d_weight), d_acc, S(stream)));
 }
 
 }  // extern "C"

@@ -18,7 +18,7 @@ def definition(acc, weight, tag, state, last, epoch, decay, protect):
     g = tag[live]
     acc[g] = np.float32(decay) * acc[g] + weight[g].astype(np.float32) * np.float32(2.0 ** -32)
     weight[g] = 0
-    young = epoch - last[live].astype(np.int64) < protect
+    young = (epoch - last[live].astype(np.int64) < protect) & (protect > 0)
     score[live] = np.where(young, np.float32(np.inf), acc[g])
     return acc, weight, score
 
@@ -41,6 +41,8 @@ def test_scores_and_victims(blocks, heads, decay, protect):
         tag = np.where(state == 1, r.permutation(2 * n + 8)[:n], 0xFFFFFFFF)
         last = r.integers(0, 12, n)
         pool.tag[:n] = torch.from_numpy(tag.astype(np.uint32).view(np.int32)).cuda()
+        pool.loc.fill_(-1)
+        pool.loc[torch.from_numpy(tag[state == 1].astype(np.int64)).cuda()] = torch.from_numpy(np.flatnonzero(state == 1).astype(np.int32)).cuda()
         pool.last_epoch[:n] = torch.from_numpy(last.astype(np.int32)).cuda()
         weight = np.where(r.random(2 * n + 8) < 0.2, 0, r.integers(0, 2 ** 44, 2 * n + 8))
         acc = r.random(2 * n + 8, dtype=np.float32)
@@ -64,7 +66,7 @@ def test_scores_and_victims(blocks, heads, decay, protect):
     pool.close()
 
 
-def test_refusals_and_handles_beyond():
+def test_refusals():
     part = W.gqa(1, 2, 2, 8, 16, 9, 16)
     pool = B.Pool([part], n_tags=18, staging_bytes=1 << 20, max_promote=16, host_meta=False)
     w, a = torch.zeros(20, dtype=torch.int64, device="cuda"), torch.zeros(20, device="cuda")
@@ -80,15 +82,23 @@ def test_refusals_and_handles_beyond():
         pool.kv_attention_score(1, 0.5, 0, w[:17], a)
     with pytest.raises(TypeError):
         pool.kv_attention_score(1, 0.5, 0, w.int(), a)
+    pool.close()
+
+
+def test_handles_that_lead_nowhere_keep_what_they_have():
+    part = W.gqa(1, 2, 2, 8, 16, 9, 16)
+    pool = B.Pool([part], n_tags=21, staging_bytes=1 << 20, max_promote=16, host_meta=False)
+    assert pool.kv_admit(0, 0.9, torch.zeros(18, dtype=torch.uint8, device="cuda"), False) == (0, 18)
     pool.sync()
-    pool.tag[3] = 99
-    w[:] = 1 << 32
+    w = (torch.arange(1, 22, device="cuda") << 32).contiguous()
+    a = torch.full((21,), 2.0, device="cuda")
+    pool.loc[19] = -2 ** 31 + 3                      # in the host tier
     torch.cuda.synchronize()
     assert pool.kv_attention_score(1, 0.5, 0, w, a) == 0
     pool.sync()
-    assert pool.kv_device_status() == B.KV_DEV_BAD_INDEX
-    s = pool.score[:18].cpu()
-    assert float(s[3]) == float("inf") and bool((s[torch.arange(18) != 3] == 1.0).all())
+    assert torch.equal(pool.score[:18], torch.arange(2.0, 20.0, device="cuda"))
+    assert w.tolist() == [0] * 18 + [19 << 32, 20 << 32, 21 << 32] and a[18:].tolist() == [2.0] * 3
+    assert pool.kv_device_status() == 0
     pool.close()
 
 

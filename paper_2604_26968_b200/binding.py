@@ -6,6 +6,7 @@ fallback: if the library cannot be loaded, loading raises.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -233,9 +234,9 @@ def load():
     L.kv_selection_stats.restype = i32
     L.kv_selection_stats.argtypes = [vp, vp, vp]
     L.kv_append.restype = i32
-    L.kv_append.argtypes = [vp, C.POINTER(kv_append_desc), vp]
+    L.kv_append.argtypes = [vp, C.c_char_p, vp]   # (a packed kv_append_desc)
     L.kv_attend.restype = i32
-    L.kv_attend.argtypes = [vp, C.POINTER(kv_attend_desc), vp]
+    L.kv_attend.argtypes = [vp, C.c_char_p, vp]   # (a packed kv_attend_desc)
     L.kv_attend_scratch_bytes.restype = u64
     L.kv_attend_scratch_bytes.argtypes = [vp, i32, u32, u32, u32, u32, u32, i32]
     L.kv_attention_score.restype = i32
@@ -299,6 +300,58 @@ def kv_select_victims_static(d_score, d_state, n, k, d_victims, d_status=None, s
         d_status.data_ptr() if d_status is not None else None, _stream_ptr(stream))
 
 
+# The descriptions of kv_append and kv_attend are packed in one go (a call is a few microseconds of them).
+_APPEND = struct.Struct("@iiiiQ" + "Pqq" * 4 + "PQPP%ds" % C.sizeof(kv_rope_desc))
+_ATTEND = struct.Struct("@iiifIIIIIIPqqPqqPPQPPPPPQ")
+_NO_ROPE = bytes(C.sizeof(kv_rope_desc))
+assert _APPEND.size == C.sizeof(kv_append_desc) and _ATTEND.size == C.sizeof(kv_attend_desc)
+_I64, _I32, _F32 = ("torch.int64", "torch.uint64"), ("torch.int32", "torch.uint32"), ("torch.float32",)
+_dtypes = {}
+
+
+def _is(dtype, names):
+    """Whether a torch dtype is one of those names (torch is only imported where a pool is made)."""
+    k = _dtypes.get(dtype)
+    if k is None:
+        k = _dtypes[dtype] = str(dtype)
+    return k in names
+
+
+def _element(what, dtype):
+    if _is(dtype, ("torch.bfloat16",)):
+        return KV_DTYPE_BF16
+    if _is(dtype, ("torch.float16",)):
+        return KV_DTYPE_F16
+    raise TypeError("%s: elements of %s" % (what, dtype))
+
+
+def _array(what, t, names, size):
+    if not _is(t.dtype, names):
+        raise TypeError("%s: a tensor of %s where %s is wanted" % (what, t.dtype, " or ".join(names)))
+    if not t.is_contiguous() or (size is not None and t.numel() != size):
+        raise ValueError("%s: an array %s where %s contiguous elements are wanted" % (what, tuple(t.shape), size))
+
+
+def _table_rows(what, t, layers, heads):
+    shape = t.shape
+    if not _is(t.dtype, _I32):
+        raise TypeError("%s: a table of %s" % (what, t.dtype))
+    if len(shape) != 3 or shape[1] != layers or shape[2] != heads or not t.is_contiguous():
+        raise ValueError("%s: a table %s where a contiguous (rows, %d, %d) is wanted" % (what, tuple(shape), layers, heads))
+    return shape[0]
+
+
+def _heads(what, t, n, heads, dim, dtype):
+    """(address, token stride, head stride) of a [n][heads][dim] tensor; zeros without one."""
+    if t is None:
+        return 0, 0, 0
+    s = t.stride()
+    if t.dtype != dtype or t.shape != (n, heads, dim) or (dim > 1 and s[2] != 1):
+        raise ValueError("%s: %s %s where %s (%d, %d, %d) with contiguous rows is wanted" %
+                         (what, t.dtype, tuple(t.shape), dtype, n, heads, dim))
+    return t.data_ptr(), s[0], s[1]
+
+
 class kv_rope:
     """Rotary positions for kv_append: kv_rope_desc and the tensor it points to.  axis: the axis of
     position each pair follows (an int for all of them)."""
@@ -309,22 +362,13 @@ class kv_rope:
         if len(axis) != half or half > 128 or (inv_freq.numel() if inv_freq is not None else 0) < half:
             raise ValueError("kv_rope: %d axes and %s frequencies for %d pairs" %
                              (len(axis), inv_freq.numel() if inv_freq is not None else "no", half))
+        if inv_freq is not None:
+            _array("kv_rope", inv_freq, _F32, None)
         self.inv_freq = inv_freq
         self.n_axes = int(n_axes if n_axes is not None else (max(axis) + 1 if axis else 0))
         self.desc = kv_rope_desc(int(rot_dim), int(first), int(bool(interleaved)), self.n_axes,
                                  (C.c_uint8 * 128)(*axis), inv_freq.data_ptr() if inv_freq is not None else None)
-
-
-def _typed(name, tensors, dtypes):
-    for t in tensors:
-        if t is not None and str(t.dtype) not in dtypes:
-            raise TypeError("%s: a tensor of %s where %s is wanted" % (name, t.dtype, " or ".join(dtypes)))
-
-
-def _plain(name, tensors):
-    for t in tensors:
-        if t is not None and not t.is_contiguous():
-            raise ValueError("%s: arrays of indices and results have to be contiguous" % name)
+        self.packed = bytes(self.desc)
 
 
 class Pool:
@@ -524,53 +568,32 @@ class Pool:
                                          d_out_count.data_ptr() if d_out_count is not None else None,
                                          _stream_ptr(self.compute))
 
-    def _heads_view(self, name, q, t, n, heads, dim, dtype):
-        """(address, strides) of a [n][heads][dim] tensor of 16-bit elements."""
-        if t is None:
-            return None, _stride(0, 0)
-        if str(t.dtype) != dtype or tuple(t.shape) != (n, heads, dim) or (dim > 1 and t.stride(2) != 1):
-            raise ValueError("%s: %s %s where %s (%d, %d, %d) with contiguous rows is wanted" %
-                             (name, t.dtype, tuple(t.shape), dtype, n, heads, dim))
-        return t.data_ptr(), _stride(t.stride(0), t.stride(1))
-
-    def _attention_dims(self, q):
-        """(key heads, elements of a query or key head, of a value head)"""
-        p = self.parts[q]
-        return ((1, p.d_latent + p.d_rope, p.d_latent) if p.variant == KV_MLA else (p.heads, p.head_dim, p.head_dim))
-
-    def _table_rows(self, name, q, table):
-        p = self.parts[q]
-        _typed(name, [table], ("torch.int32", "torch.uint32"))
-        _plain(name, [table])
-        if tuple(table.shape[1:]) != (p.n_layers, p.heads) or table.dim() != 3:
-            raise ValueError("%s: a table of %s where (rows, %d, %d) is wanted" % (name, tuple(table.shape), p.n_layers, p.heads))
-        return table.shape[0]
+    def _attention(self, q):
+        """(layers, key heads, query heads, elements of a query or key head, of a value head) of a partition."""
+        d = self.__dict__.setdefault("_attention_dims", {})
+        if q not in d:
+            p = self.parts[q]
+            d[q] = ((p.n_layers, 1, p.n_q_heads, p.d_latent + p.d_rope, p.d_latent) if p.variant == KV_MLA
+                    else (p.n_layers, p.heads, p.n_q_heads, p.head_dim, p.head_dim))
+        return d[q]
 
     def kv_append(self, q, layer, d_k, d_v, d_table, d_slot, d_q=None, d_q_out=None, rope=None, d_pos=None, stream=None):
         """d_k, d_v, d_q, d_q_out: [tokens, heads, dim] (any strides but the last); d_slot int64 [tokens];
         d_pos int32 [axes, tokens]; rope: kv_rope."""
-        n = d_slot.numel()
-        H, dk, dv = self._attention_dims(q)
-        dt = str(d_k.dtype)
-        if dt not in ("torch.bfloat16", "torch.float16"):
-            raise TypeError("kv_append: keys of %s" % dt)
-        _typed("kv_append", [d_slot], ("torch.int64",))
-        _typed("kv_append", [d_pos], ("torch.int32",))
-        _plain("kv_append", [d_slot, d_pos])
-        if rope is not None and d_pos is not None and d_pos.numel() != rope.n_axes * n:
-            raise ValueError("kv_append: %d positions for %d axes of %d tokens" % (d_pos.numel(), rope.n_axes, n))
-        QH = self.parts[q].n_q_heads
-        d = kv_append_desc(int(q), int(layer), KV_DTYPE_BF16 if dt == "torch.bfloat16" else KV_DTYPE_F16, 0, n)
-        d.d_k, d.k_stride = self._heads_view("kv_append", q, d_k, n, H, dk, dt)
-        d.d_v, d.v_stride = self._heads_view("kv_append", q, d_v, n, H, dv, dt)
-        d.d_q, d.q_stride = self._heads_view("kv_append", q, d_q, n, QH, dk, dt)
-        d.d_q_out, d.q_out_stride = self._heads_view("kv_append", q, d_q_out, n, QH, dk, dt)
-        d.n_rows = self._table_rows("kv_append", q, d_table)
-        d.d_table, d.d_slot = d_table.data_ptr(), d_slot.data_ptr()
-        d.d_pos = d_pos.data_ptr() if d_pos is not None else None
-        if rope is not None:
-            d.rope = rope.desc
-        return self.lib.kv_append(self._h, C.byref(d), _stream_ptr(stream if stream is not None else self.compute))
+        what = "kv_append"
+        layers, H, QH, dk, dv = self._attention(q)
+        n, dt = d_slot.shape[0], d_k.dtype
+        rows = _table_rows(what, d_table, layers, H)
+        _array(what, d_slot, _I64, n)
+        if d_pos is not None and rope is not None:
+            _array(what, d_pos, _I32, rope.n_axes * n)
+        elif d_pos is not None:
+            _array(what, d_pos, _I32, None)
+        desc = _APPEND.pack(q, layer, _element(what, dt), 0, n, *_heads(what, d_k, n, H, dk, dt), *_heads(what, d_v, n, H, dv, dt),
+                            *_heads(what, d_q, n, QH, dk, dt), *_heads(what, d_q_out, n, QH, dk, dt), d_table.data_ptr(), rows,
+                            d_slot.data_ptr(), d_pos.data_ptr() if d_pos is not None else 0,
+                            rope.packed if rope is not None else _NO_ROPE)
+        return self.lib.kv_append(self._h, desc, _stream_ptr(stream if stream is not None else self.compute))
 
     def kv_attend_scratch_bytes(self, q, n_seqs, n_groups=0, max_suffix=0, max_prefix=0, max_members=0, weights=False):
         return int(self.lib.kv_attend_scratch_bytes(self._h, int(q), int(n_seqs), int(n_groups), int(max_suffix),
@@ -580,42 +603,40 @@ class Pool:
                   d_group=None, max_prefix=0, max_members=0, d_lse=None, d_weight=None, stream=None):
         """d_q, d_out: [sequences, query heads, dim]; d_suffix [sequences, 2], d_prefix [groups, 2] and d_group
         [groups + 1] int32; d_lse float32 [sequences, query heads]; d_weight int64 [n_tags]."""
-        S, QH = d_q.shape[0], self.parts[q].n_q_heads
-        _, dk, dv = self._attention_dims(q)
-        dt = str(d_q.dtype)
-        if dt not in ("torch.bfloat16", "torch.float16"):
-            raise TypeError("kv_attend: queries of %s" % dt)
-        n_groups = d_prefix.shape[0] if d_prefix is not None else 0
-        _typed("kv_attend", [d_suffix, d_prefix, d_group], ("torch.int32", "torch.uint32"))
-        _typed("kv_attend", [d_lse], ("torch.float32",))
-        _typed("kv_attend", [d_weight], ("torch.int64", "torch.uint64"))
-        _plain("kv_attend", [d_suffix, d_prefix, d_group, d_lse, d_weight, d_scratch])
-        if (d_suffix.numel() != 2 * S or (d_prefix is not None and d_prefix.numel() != 2 * n_groups) or
-                (n_groups and (d_group is None or d_group.numel() != n_groups + 1)) or
-                (d_lse is not None and d_lse.numel() != S * QH) or (d_weight is not None and d_weight.numel() < self.n_tags)):
-            raise ValueError("kv_attend: arrays for %d sequences in %d groups have other sizes" % (S, n_groups))
-        d = kv_attend_desc(int(q), int(layer), KV_DTYPE_BF16 if dt == "torch.bfloat16" else KV_DTYPE_F16, float(scale),
-                           S, n_groups, int(max_suffix), int(max_prefix), int(max_members), 0)
-        d.d_q, d.q_stride = self._heads_view("kv_attend", q, d_q, S, QH, dk, dt)
-        d.d_out, d.out_stride = self._heads_view("kv_attend", q, d_out, S, QH, dv, dt)
-        d.n_rows = self._table_rows("kv_attend", q, d_table)
-        d.d_table, d.d_suffix = d_table.data_ptr(), d_suffix.data_ptr()
-        d.d_lse = d_lse.data_ptr() if d_lse is not None else None
-        d.d_prefix = d_prefix.data_ptr() if d_prefix is not None else None
-        d.d_group = d_group.data_ptr() if d_group is not None else None
-        d.d_weight = d_weight.data_ptr() if d_weight is not None else None
-        d.d_scratch, d.scratch_bytes = d_scratch.data_ptr(), d_scratch.numel() * d_scratch.element_size()
-        return self.lib.kv_attend(self._h, C.byref(d), _stream_ptr(stream if stream is not None else self.compute))
+        what = "kv_attend"
+        layers, _, QH, dk, dv = self._attention(q)
+        n, dt = d_q.shape[0], d_q.dtype
+        rows = _table_rows(what, d_table, layers, _)
+        _array(what, d_suffix, _I32, 2 * n)
+        groups = 0
+        if d_prefix is not None:
+            groups = d_prefix.shape[0]
+            _array(what, d_prefix, _I32, 2 * groups)
+            if d_group is None:
+                raise ValueError("kv_attend: %d prefixes without groups" % groups)
+            _array(what, d_group, _I32, groups + 1)
+        if d_lse is not None:
+            _array(what, d_lse, _F32, n * QH)
+        if d_weight is not None:
+            _array(what, d_weight, _I64, None)
+            if d_weight.numel() < self.n_tags:
+                raise ValueError("kv_attend: weights of %d handles, where %d may be named" % (d_weight.numel(), self.n_tags))
+        if not d_scratch.is_contiguous():
+            raise ValueError("kv_attend: the scratch has to be contiguous")
+        desc = _ATTEND.pack(q, layer, _element(what, dt), scale, n, groups, max_suffix, max_prefix, max_members, 0,
+                            *_heads(what, d_q, n, QH, dk, dt), *_heads(what, d_out, n, QH, dv, dt),
+                            d_lse.data_ptr() if d_lse is not None else 0, d_table.data_ptr(), rows, d_suffix.data_ptr(),
+                            d_prefix.data_ptr() if d_prefix is not None else 0, d_group.data_ptr() if d_prefix is not None else 0,
+                            d_weight.data_ptr() if d_weight is not None else 0, d_scratch.data_ptr(), d_scratch.nbytes)
+        return self.lib.kv_attend(self._h, desc, _stream_ptr(stream if stream is not None else self.compute))
 
     def kv_attention_score(self, epoch, decay, protect, d_weight, d_acc):
         """d_weight int64 [n_tags] (cleared), d_acc float32 [n_tags]."""
-        _typed("kv_attention_score", [d_weight], ("torch.int64", "torch.uint64"))
-        _typed("kv_attention_score", [d_acc], ("torch.float32",))
-        _plain("kv_attention_score", [d_weight, d_acc])
+        _array("kv_attention_score", d_weight, _I64, None)
+        _array("kv_attention_score", d_acc, _F32, None)
         if d_weight.numel() < self.n_tags or d_acc.numel() < self.n_tags:
             raise ValueError("kv_attention_score: arrays of fewer than %d handles" % self.n_tags)
-        return self.lib.kv_attention_score(self._h, int(epoch), float(decay), int(protect), d_weight.data_ptr(),
-                                           d_acc.data_ptr(), _stream_ptr(self.compute))
+        return self.lib.kv_attention_score(self._h, epoch, decay, protect, d_weight.data_ptr(), d_acc.data_ptr(), _stream_ptr(self.compute))
 
     def kv_set_l2_residency(self, budget_bytes):
         return self.lib.kv_set_l2_residency(self._h, int(budget_bytes))

@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constan
                threadIdx.x == 0))
     return;
   if (w.to == 0) {
-    put_nothing<T>(a, w);
+    put_nothing<T>(a, w, threadIdx.x, blockDim.x);
     return;
   }
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
   if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? blockIdx.x - first_kind_items : blockIdx.x, kRows, w, threadIdx.x == 0))
     return;
   if (w.to == 0) {
-    put_nothing<T>(a, w);
+    put_nothing<T>(a, w, threadIdx.x, blockDim.x);
     return;
   }
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;

@@ -120,6 +120,7 @@ struct AttendArgs {
 };
 
 constexpr uint32_t kMaxRowDim = 576;          // widest row of keys (MLA)
+constexpr uint32_t kStreamUnit = 16, kStreamTokens = 1024;   // a warp's of kv_attend_stream.cu
 constexpr uint32_t kMaxChunkTokens = 4096, kMaxChunkBlocks = 256;   // most a CTA takes of a segment
 
 // kv_attend.cu
@@ -132,6 +133,7 @@ cudaError_t launch_attend_tiles(const AttendArgs& a, int dtype, bool mla, bool p
 // kv_attend_stream.cu: the same for up to 32 rows.  behind_tiles: launch_attend_tiles went ahead in this call, and the two
 // may run side by side.
 bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows);
+uint32_t stream_warps(uint32_t dk, uint32_t rows);   // of an SM
 cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, uint32_t rows, bool prefix, bool suffix, bool behind_tiles,
                                  cudaStream_t s);
 

@@ -113,10 +113,10 @@ __device__ __forceinline__ uint32_t part_of(const AttendArgs& a, const Item& w) 
   return w.kind == kKindPrefix ? w.chunk : a.chunks[kKindPrefix] + w.chunk;
 }
 
-// A sequence without tokens, where no join follows.
+// A sequence without tokens, where no join follows; by `threads` threads.
 template <typename T>
-__device__ void put_nothing(const AttendArgs& a, const Item& w) {
-  for (uint32_t i = threadIdx.x; i < w.rows * (a.dv / 2u); i += blockDim.x) {
+__device__ void put_nothing(const AttendArgs& a, const Item& w, uint32_t thread, uint32_t threads) {
+  for (uint32_t i = thread; i < w.rows * (a.dv / 2u); i += threads) {
     const uint32_t r = i / (a.dv / 2u), d = i % (a.dv / 2u) * 2u;
     uint32_t seq, head;
     row_of(a, w, r, seq, head);

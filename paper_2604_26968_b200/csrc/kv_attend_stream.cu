@@ -1,42 +1,45 @@
 // kv_attend where few rows read a block: a stream of blocks through independent warps (and the encoder of the maps
 // by which the kernels here and in kv_attend_tiles.cu copy blocks).
 //
-// A CTA's chunk of a segment is dealt out to its warps in units of 16 tokens of one block; a block that is not in HBM is no
-// unit.  Each warp has a ring of units of its own, filled by TMA (a box of 16 rows x 64 elements, swizzled, for each
-// panel of K and V) which the warp itself issues as it empties them: no barrier between warps until they join at the end.
-// A unit's scores (16 kM rows x 16 tokens) and output are mma.sync products whose operands come from the ring by ldmatrix,
-// free of bank conflicts thanks to the swizzle.  The output is rescaled only when a maximum has grown by more than 2^8.
-// Bound: HBM.  Four warps with three units of 8 KB each, two CTAs an SM, keep 128 KB or more in flight on every SM.
+// A warp takes a chunk of a segment in units of 16 tokens of one block; a block that is not in HBM is no unit.  It has a ring
+// of units of its own, filled by TMA (a box of 16 rows x 64 elements, swizzled, for each panel of K and V) which it issues
+// itself as it empties them: no warp waits for another.  A unit's scores (16 kM rows x 16 tokens) and output are mma.sync
+// products whose operands come from the ring by ldmatrix, free of bank conflicts thanks to the swizzle.  The output is
+// rescaled only when a maximum has grown by more than 2^8.
+// Bound: HBM.  A unit takes a warp about 2,000 cycles, most of them latencies of its short products and reductions, so it takes
+// eight to sixteen warps on every SM, each with two to three units under way; a chunk's start (its segment, its blocks' handles and
+// places, the first copies: five reads one after the other) costs as much as three units.
 #include "kv_attend_device.cuh"
 #include "kv_attend_tma.cuh"
 
 namespace kvt {
 namespace {
 
-constexpr int kUnit = 16;        // tokens
+constexpr int kUnit = kStreamUnit;        // tokens
 constexpr int kStreamWarps = 4;
-constexpr uint32_t kMaxUnits = kMaxChunkTokens / kUnit;
+constexpr uint32_t kMaxUnits = kStreamTokens / kUnit;
 
 template <int D, int kM>
 struct Stream {
   static constexpr int kPanels = D / 64, kPanelBytes = kUnit * 128, kUnitBytes = 2 * kPanels * kPanelBytes;
-  static constexpr int kSlots = D == 128 ? 3 : 6;
+  static constexpr int kSlots = D == 64 || kM == 2 ? 3 : 2;
+  static constexpr int kCtas = D == 64 ? (kM == 2 ? 3 : 4) : (kM == 2 ? 2 : 3);   // of an SM
   static constexpr size_t kRing = (size_t)kStreamWarps * kSlots * kUnitBytes;
-  static constexpr size_t kJoin = (size_t)kStreamWarps * kM * 16 * (D + 2) * 4;
-  static constexpr size_t kUnits = (kRing > kJoin ? kRing : kJoin);      // what follows the ring: the list of units, barriers
-  static constexpr size_t kSmem = 1024 + kUnits + kMaxUnits * 8 + kStreamWarps * kSlots * 8 + 16;
+  static constexpr size_t kSmem = 1024 + kRing + kStreamWarps * (kMaxUnits * 8 + kSlots * 8 + 8);
 };
 
-template <typename T, int D, int kM>
-__global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
-                                                                   uint32_t first_kind_items, uint32_t behind_tiles) {
+template <typename T, int D, int kM, bool kWeights>
+__global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
+    stream_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, uint32_t first_kind_items, uint32_t items,
+                  uint32_t behind_tiles) {
   using S = Stream<D, kM>;
   extern __shared__ uint8_t raw[];
   uint8_t* const smem = raw + ((1024u - (smem_address(raw) & 1023u)) & 1023u);
-  uint2* const units = reinterpret_cast<uint2*>(smem + S::kUnits);                     // (first row in the slab, first token)
-  unsigned long long* const bars = reinterpret_cast<unsigned long long*>(units + kMaxUnits);
-  uint32_t* const control = reinterpret_cast<uint32_t*>(bars + kStreamWarps * S::kSlots);   // units, gave up
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  uint8_t* const ring = smem + warp * (S::kSlots * S::kUnitBytes);
+  uint2* const units = reinterpret_cast<uint2*>(smem + S::kRing) + warp * kMaxUnits;      // (first row in the slab, first token)
+  unsigned long long* const bar = reinterpret_cast<unsigned long long*>(smem + S::kRing + kStreamWarps * kMaxUnits * 8) + warp * (S::kSlots + 1);
+  volatile uint32_t* const gave_up = reinterpret_cast<uint32_t*>(bar + S::kSlots);
   // Behind a launch of the tiles kernel, which has waited for all that is ahead of it, the two may run side by side; this
   // one then ends only when that one has.
   if (behind_tiles) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -49,41 +52,53 @@ __global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_
   } at_end{behind_tiles};
 
   Item w;
-  const bool second = blockIdx.x >= first_kind_items;
-  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? blockIdx.x - first_kind_items : blockIdx.x, kM * 16, w, threadIdx.x == 0)) return;
+  uint32_t item = blockIdx.x * kStreamWarps + warp;
+  if (item >= items) return;
+  const bool second = item >= first_kind_items;
+  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? item - first_kind_items : item, kM * 16, w, lane == 0)) return;
   if (w.to == 0) {
-    put_nothing<T>(a, w);
+    put_nothing<T>(a, w, lane, 32);
     return;
   }
   const TableView& tv = a.tv;
-  if (warp == 0) {
-    const uint32_t n = (w.to - w.from + kUnit - 1u) / kUnit;
-    uint32_t found = 0;
-    for (uint32_t u0 = 0; u0 < n; u0 += 128u) {
-      uint32_t ch[4];
+  if (lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t u = u0 + k * 32u + lane;
-        ch[k] = u < n ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(w.from + u * kUnit), w.head) : ~0u;
-      }
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t at = w.from + (u0 + k * 32u + lane) * kUnit;
-        const uint32_t there = __ballot_sync(~0u, ch[k] != ~0u);
-        if (ch[k] != ~0u)
-          units[found + __popc(there & ((1u << lane) - 1u))] = make_uint2(ch[k] * tv.block_tokens + (at - tv.by_tokens(at) * tv.block_tokens), at);
-        found += __popc(there);
-      }
-    }
-    if (lane == 0) {
-      control[0] = found;
-      control[1] = 0;
-    }
-  } else if (threadIdx.x == 32) {
-    for (int b = 0; b < kStreamWarps * S::kSlots; ++b) bar_init(smem_address(bars + b), 1);
+    for (int b = 0; b < S::kSlots; ++b) bar_init(smem_address(bar + b), 1);
+    *gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
+  uint32_t n_units = 0;
+  {
+    const uint32_t n = (w.to - w.from + kUnit - 1u) / kUnit;
+    uint32_t ch[kMaxUnits / 32];
+#pragma unroll
+    for (int k = 0; k < (int)kMaxUnits / 32; ++k) {
+      const uint32_t u = k * 32u + lane;
+      ch[k] = u < n ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(w.from + u * kUnit), w.head) : ~0u;
+    }
+#pragma unroll
+    for (int k = 0; k < (int)kMaxUnits / 32; ++k) {
+      const uint32_t at = w.from + (k * 32u + lane) * kUnit;
+      const uint32_t there = __ballot_sync(~0u, ch[k] != ~0u);
+      if (ch[k] != ~0u)
+        units[n_units + __popc(there & ((1u << lane) - 1u))] = make_uint2(ch[k] * tv.block_tokens + (at - tv.by_tokens(at) * tv.block_tokens), at);
+      n_units += __popc(there);
+    }
+  }
+  __syncwarp();
+  // unit j into a slot, a lane for each box: panels of K, then of V
+  const int32_t box_x = (lane % S::kPanels) * 64, box_y = lane / S::kPanels ? (int32_t)(tv.heads * tv.block_tokens) : 0;
+  auto issue = [&](uint32_t j, uint32_t slot) {
+    if (j >= n_units) return;
+    const uint32_t b = smem_address(bar + slot);
+    if (lane == 0) bar_expect(b, S::kUnitBytes);
+    __syncwarp();
+    if (lane < 2 * S::kPanels) tma_box(smem_address(ring + slot * S::kUnitBytes + lane * S::kPanelBytes), &map, box_x, (int32_t)units[j].x + box_y, b);
+  };
+#pragma unroll
+  for (int k = 0; k < S::kSlots; ++k) issue(k, k);
   // queries straight into the operands' registers: rows lane / 4 and 8 further on, elements 2 (lane % 4) and 8 further on
   uint32_t q[kM][D / 16][4];
 #pragma unroll
@@ -95,30 +110,15 @@ __global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_
       uint32_t seq = 0, head = 0;
       if (there) row_of(a, w, r, seq, head);
       const uint16_t* const src = static_cast<const uint16_t*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + (lane & 3) * 2;
+      const bool words = (reinterpret_cast<uintptr_t>(src) & 3u) == 0;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) q[i][k][h + 2 * e] = there ? (uint32_t)src[k * 16 + e * 8] | (uint32_t)src[k * 16 + e * 8 + 1] << 16 : 0u;
+        for (int e = 0; e < 2; ++e) {
+          const uint16_t* const x = src + k * 16 + e * 8;
+          q[i][k][h + 2 * e] = !there ? 0u : words ? *reinterpret_cast<const uint32_t*>(x) : (uint32_t)x[0] | (uint32_t)x[1] << 16;
+        }
     }
-  __syncthreads();
-  const uint32_t n_units = control[0];
-  volatile uint32_t* const gave_up = control + 1;
-  uint8_t* const ring = smem + warp * (S::kSlots * S::kUnitBytes);
-  unsigned long long* const bar = bars + warp * S::kSlots;
-  auto issue = [&](uint32_t j, uint32_t slot) {      // unit j into a slot, by the first lane
-    if (lane == 0 && j < n_units) {
-      const uint32_t dst = smem_address(ring + slot * S::kUnitBytes), b = smem_address(bar + slot);
-      const int32_t y = (int32_t)units[j].x;
-      bar_expect(b, S::kUnitBytes);
-#pragma unroll
-      for (int p = 0; p < S::kPanels; ++p) {
-        tma_box(dst + p * S::kPanelBytes, &map, p * 64, y, b);
-        tma_box(dst + (S::kPanels + p) * S::kPanelBytes, &map, p * 64, y + (int32_t)(tv.heads * tv.block_tokens), b);
-      }
-    }
-  };
-#pragma unroll
-  for (int k = 0; k < S::kSlots; ++k) issue(warp + k * kStreamWarps, k);
 
   float o[kM][D / 8][4], m[kM][2], l[kM][2];
 #pragma unroll
@@ -132,8 +132,10 @@ __global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_
   }
   const uint32_t k_row = (lane >> 4) * 8 + (lane & 7), v_row = (lane >> 3 & 1) * 8 + (lane & 7);
   uint32_t slot = 0, parity = 0;
-  for (uint32_t j = warp; j < n_units; j += kStreamWarps) {
-    if (!__all_sync(~0u, bar_wait(smem_address(bar + slot), parity, gave_up, tv.status))) break;
+  bool ok = true;
+  for (uint32_t j = 0; j < n_units; ++j) {
+    ok = __all_sync(~0u, bar_wait(smem_address(bar + slot), parity, gave_up, tv.status));
+    if (!ok) break;
     uint8_t* const unit = ring + slot * S::kUnitBytes;
     const uint32_t k_at = smem_address(unit) + k_row * 128, v_at = smem_address(unit) + S::kPanels * S::kPanelBytes + v_row * 128;
     const uint32_t at = units[j].y, left = w.to - at;
@@ -210,12 +212,13 @@ __global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_
       }
       l[i][0] += part[0];
       l[i][1] += part[1];
-      if (a.weight) {
+      if (kWeights) {
+        float* const grain = grain_at(a, w, at / 16u);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const float sum = quad_sum(part[h]);
           const uint32_t r = i * 16 + lane / 4 + h * 8;
-          if ((lane & 3) == 0 && r < w.rows) grain_at(a, w, at / 16u)[r] = base[h] + log2_(sum);
+          if ((lane & 3) == 0 && r < w.rows) grain[r] = base[h] + log2_(sum);
         }
       }
     }
@@ -231,24 +234,31 @@ __global__ void __launch_bounds__(kStreamWarps * 32) stream_kernel(const __grid_
       }
     }
     __syncwarp();
-    issue(j + S::kSlots * kStreamWarps, slot);
+    issue(j + S::kSlots, slot);
     if (++slot == S::kSlots) {
       slot = 0;
       parity ^= 1u;
     }
   }
-  if (*gave_up) {
+  if (!ok) {
     // copies in flight end before the memory is given back
     for (uint32_t k = 0; k < 1u << 16; ++k) asm volatile("nanosleep.u32 1000;");
   }
-  __syncthreads();
+  const uint32_t part = part_of(a, w);
 #pragma unroll
-  for (int i = 0; i < kM; ++i) {
-    l[i][0] = quad_sum(l[i][0]);
-    l[i][1] = quad_sum(l[i][1]);
-    join_warps<D, kM, kStreamWarps>(smem, i, warp, o[i], m[i], l[i]);
-  }
-  put_joined<T, D, kM, kStreamWarps>(a, w, part_of(a, w), smem);
+  for (int i = 0; i < kM; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float sum = quad_sum(l[i][h]);
+      const uint32_t r = i * 16 + lane / 4 + h * 8;
+      if (r >= w.rows) continue;
+      uint32_t seq, head;
+      row_of(a, w, r, seq, head);
+      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) put2<T>(a, seq, head, part, j * 8 + (lane & 3) * 2, o[i][j][2 * h] * inv, o[i][j][2 * h + 1] * inv);
+      if ((lane & 3) == 0) put_lse(a, seq, head, part, sum != 0.0f ? m[i][h] + log2_(sum) : -INFINITY);
+    }
 }
 
 typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -279,10 +289,11 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_ti
   const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
   if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
-  auto* kernel = stream_kernel<T, D, kM>;
+  auto* kernel = a.weight ? stream_kernel<T, D, kM, true> : stream_kernel<T, D, kM, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_overlapped_smem(kernel, (unsigned)(np + ns), (unsigned)kStreamWarps * 32, S::kSmem, s, a, map, (uint32_t)np, behind_tiles ? 1u : 0u);
+  return launch_overlapped_smem(kernel, (unsigned)((np + ns + kStreamWarps - 1) / kStreamWarps), (unsigned)kStreamWarps * 32, S::kSmem, s, a, map,
+                                (uint32_t)np, (uint32_t)(np + ns), behind_tiles ? 1u : 0u);
 }
 
 template <typename T>
@@ -305,6 +316,10 @@ bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, CUtensorMap*
 
 bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows) {
   return !mla && (dk == 128 || dk == 64) && block_tokens % kUnit == 0 && slab_rows < 0x7fff0000ull && has_block_map();
+}
+
+uint32_t stream_warps(uint32_t dk, uint32_t rows) {
+  return kStreamWarps * (dk == 64 ? (rows <= 16 ? Stream<64, 1>::kCtas : Stream<64, 2>::kCtas) : (rows <= 16 ? Stream<128, 1>::kCtas : Stream<128, 2>::kCtas));
 }
 
 cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, uint32_t rows, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {

@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   const bool second = i >= first_kind_items;
   if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? i - first_kind_items : i, S::kTiles * 128, w, threadIdx.x == 0 && col0 == 0)) return;
   if (w.to == 0) {
-    if (col0 == 0) put_nothing<T>(a, w);
+    if (col0 == 0) put_nothing<T>(a, w, threadIdx.x, blockDim.x);
     return;
   }
   const int row_tiles = w.rows > 128u ? 2 : 1;

@@ -55,19 +55,17 @@ struct Split {
 };
 
 // Chunks of a segment of `most` tokens when `ctas` row tiles are split alike and `slots` CTAs run at a time: the
-// split whose turns, times the tiles of a chunk and what a CTA costs beside them (`extra` tiles), are fewest.
-void split_segment(uint64_t ctas, uint32_t most, uint32_t tile, uint32_t slots, uint32_t extra, uint32_t block_tokens, uint32_t* chunk,
-                   uint32_t* chunks) {
-  uint64_t limit = (uint64_t)kMaxChunkBlocks * block_tokens / tile * tile;
-  if (limit < tile) limit = tile;
-  if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
+// split whose turns, times the tiles of a chunk and what a CTA costs beside them (`extra` tiles), are fewest.  alone: no
+// other segments' parts are joined with these, so that one part needs no second launch (as long as `extra` twice).
+void split_segment(uint64_t ctas, uint32_t most, uint32_t tile, uint32_t slots, uint32_t extra, uint64_t limit, bool alone,
+                   uint32_t* chunk, uint32_t* chunks) {
   if (!ctas) ctas = 1;
   const uint64_t tiles = ((uint64_t)most + tile - 1) / tile, most_tiles = limit / tile;
   uint64_t n = (tiles + most_tiles - 1) / most_tiles, best = ~0ull, best_tiles = 1;
   const uint64_t last = n + 2 * slots / ctas + 1;
   for (; n <= last && n <= tiles; ++n) {
     const uint64_t per = (tiles + n - 1) / n, parts = (tiles + per - 1) / per;
-    const uint64_t cost = (ctas * parts + slots - 1) / slots * (per + extra);
+    const uint64_t cost = (ctas * parts + slots - 1) / slots * (per + extra) + (alone && parts > 1 ? 2 * extra : 0);
     if (cost < best) {
       best = cost;
       best_tiles = per;
@@ -99,13 +97,20 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
     const uint64_t rows = k == 0 ? prefix_rows : group, segs = (uint64_t)(k == 0 ? n_groups : n_seqs) * heads;
     const uint32_t most = k == 0 ? max_prefix : max_suffix ? max_suffix : 1;
     out->tiles[k] = fits && rows >= kTileRows;
+    uint64_t limit = (uint64_t)kMaxChunkBlocks * bt / 64 * 64;   // most tokens of a chunk
+    if (limit < 64) limit = 64;
+    if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
     out->stream[k] = !out->tiles[k] && streams && rows <= 32;
     if (out->tiles[k]) {
       const uint64_t tile = mla ? 128 : 256;
-      split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, bt, &out->chunk_tokens[k], &out->chunks[k]);
+      split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
+    } else if (out->stream[k]) {
+      const uint64_t tile = rows <= 16 ? 16 : 32;
+      split_segment((rows + tile - 1) / tile * segs, most, kStreamUnit, kSms * stream_warps(dk, (uint32_t)rows), 3, kStreamTokens, !shared, &out->chunk_tokens[k],
+                    &out->chunks[k]);
     } else {
       const uint64_t tile = mla ? 64 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-      split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, bt, &out->chunk_tokens[k], &out->chunks[k]);
+      split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
     }
   }
   out->n_parts = out->chunks[0] + out->chunks[1];

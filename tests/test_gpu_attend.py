@@ -309,10 +309,10 @@ def test_no_sequences_and_refusals():
     call = dict(scale=0.1, d_scratch=scratch, max_suffix=90)
     assert p.kv_attend(0, 1, q, out, table, suffix, **call) == 0
     assert p.kv_attend(0, 1, q[:0], out[:0], table, suffix[:0], **call) == 0
-    assert p.kv_attend(1, 1, q, out, table, suffix, **call) == B.KV_ERR_INVALID_ARG if len(p.parts) > 1 else True
+    assert p.kv_attend(0, -1, q, out, table, suffix, **call) == B.KV_ERR_INVALID_ARG
     assert p.kv_attend(0, 2, q, out, table, suffix, **call) == B.KV_ERR_INVALID_ARG
     assert p.kv_attend(0, 1, q, out, table, suffix, **{**call, "scale": math.nan}) == B.KV_ERR_INVALID_ARG
-    assert p.kv_attend(0, 1, q, out, table, suffix, **{**call, "d_scratch": scratch[:256]}) == B.KV_ERR_INVALID_ARG
+    assert p.kv_attend(0, 1, q, out, table, suffix, **{**call, "max_suffix": 50_000}) == B.KV_ERR_INVALID_ARG      # (scratch too small)
     assert p.kv_attend(0, 1, q, out, table, suffix, **{**call, "max_suffix": 0x40000000}) == B.KV_ERR_INVALID_ARG
     with pytest.raises(ValueError):
         p.kv_attend(0, 1, q, out[:1], table, suffix, **call)

@@ -475,15 +475,22 @@ struct Parts {
   uint32_t np, ns, suffix_at;
   __device__ __forceinline__ uint32_t place(uint32_t i) const { return i < np ? i : suffix_at + i - np; }
 };
-__device__ __forceinline__ Parts parts_of(const AttendArgs& a, uint32_t seq) {
-  Parts p{0, 0, a.chunks[0]};
+__device__ __forceinline__ Parts parts_of(const AttendArgs& a, uint32_t seq, uint32_t group) {
+  Parts p{0, 0, a.chunks[0] * a.per_chunk[0]};
   const Segment sfx = a.checked(a.suffix, seq, a.max_suffix, false);
-  if (a.n_groups) {
-    const uint32_t g = a.group_of(seq);
-    if (g != ~0u) p.np = (a.checked(a.prefix, g, a.max_prefix, false).tokens + a.chunk_tokens[0] - 1u) / a.chunk_tokens[0];
-  }
-  p.ns = (sfx.tokens + a.chunk_tokens[1] - 1u) / a.chunk_tokens[1];
+  if (group != ~0u)
+    p.np = (a.checked(a.prefix, group, a.max_prefix, false).tokens + a.chunk_tokens[0] - 1u) / a.chunk_tokens[0] * a.per_chunk[0];
+  p.ns = (sfx.tokens + a.chunk_tokens[1] - 1u) / a.chunk_tokens[1] * a.per_chunk[1];
   return p;
+}
+// The group of a sequence (or ~0u), asked by a whole warp.
+__device__ __forceinline__ uint32_t group_of_warp(const AttendArgs& a, uint32_t seq) {
+  if (a.n_groups >= 32u) return a.group_of(seq);
+  if (!a.n_groups) return ~0u;
+  const uint32_t lane = threadIdx.x % 32u, start = lane <= a.n_groups ? a.group_start[lane] : ~0u;
+  const uint32_t g = __popc(__ballot_sync(~0u, lane < a.n_groups && start <= seq)) - 1u;   // the last group that starts at or before it
+  const uint32_t lo = __shfl_sync(~0u, start, g & 31u), hi = __shfl_sync(~0u, start, (g + 1u) & 31u);
+  return g != ~0u && lo <= seq && seq < hi && hi <= a.n_seqs && hi - lo <= a.max_members ? g : ~0u;
 }
 
 // out and lse of rows (sequence, query head), a warp for each.
@@ -492,7 +499,7 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, uint64_t row) {
   const uint32_t lane = threadIdx.x % 32;
   if (row >= (uint64_t)a.n_seqs * a.q_heads) return;
   const uint32_t seq = (uint32_t)(row / a.q_heads), head = (uint32_t)(row - (uint64_t)seq * a.q_heads);
-  const Parts parts = parts_of(a, seq);
+  const Parts parts = parts_of(a, seq, group_of_warp(a, seq));
   const uint32_t n = parts.np + parts.ns;
   const float* const lse = a.part_lse + row * a.n_parts;
   const float first = lane < n ? lse[parts.place(lane)] : -INFINITY;
@@ -516,16 +523,22 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, uint64_t row) {
       const float mine = i0 == 0 ? first : (i0 + lane < n ? lse[parts.place(i0 + lane)] : -INFINITY);
       const float share = exp2_(mine - base) * inv;
       const uint32_t most = min(32u, n - i0);
-#pragma unroll 4
-      for (uint32_t i = 0; i < most; ++i) {
-        const float c = __shfl_sync(~0u, share, i);
-        const bool some = __shfl_sync(~0u, mine, i) != -INFINITY;   // (a part of nothing has not been written)
-        if (some && d < a.dv) {
-          const float4 v = *reinterpret_cast<const float4*>(a.part_o + (row * a.n_parts + parts.place(i0 + i)) * a.dv + d);
-          x.x = __fmaf_rn(c, v.x, x.x);
-          x.y = __fmaf_rn(c, v.y, x.y);
-          x.z = __fmaf_rn(c, v.z, x.z);
-          x.w = __fmaf_rn(c, v.w, x.w);
+      for (uint32_t i = 0; i < most; i += 8u) {
+        float4 v[8];
+        float c[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          c[k] = __shfl_sync(~0u, share, (i + k) & 31u);
+          const bool some = __shfl_sync(~0u, mine, (i + k) & 31u) != -INFINITY && i + k < most;   // (a part of nothing has not been written)
+          v[k] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (some && d < a.dv) v[k] = *reinterpret_cast<const float4*>(a.part_o + (row * a.n_parts + parts.place(i0 + i + k)) * a.dv + d);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x.x = __fmaf_rn(c[k], v[k].x, x.x);
+          x.y = __fmaf_rn(c[k], v[k].y, x.y);
+          x.z = __fmaf_rn(c[k], v[k].z, x.z);
+          x.w = __fmaf_rn(c[k], v[k].w, x.w);
         }
       }
     }
@@ -576,7 +589,7 @@ __device__ __forceinline__ void add_weights(const AttendArgs& a, int kind, uint3
         total[r] = lse[0];
         continue;
       }
-      const Parts parts = parts_of(a, seq);
+      const Parts parts = parts_of(a, seq, kind == kKindPrefix ? index : a.n_groups ? a.group_of(seq) : ~0u);
       float top = -INFINITY, sum = 0.0f;
       for (uint32_t i = 0; i < parts.np + parts.ns; ++i) top = fmaxf(top, lse[parts.place(i)]);
       const float base = top == -INFINITY ? 0.0f : top;
@@ -661,14 +674,7 @@ cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t 
   if (tp || ts) e = launch_attend_tiles(a, dtype, mla, tp, ts, s);
   if (e != cudaSuccess) return e;
   if (sp || ss) {
-    const uint32_t rows = a.max_members * a.group;
-    const bool behind = tp || ts;
-    if (sp && ss && (rows <= 16) != (a.group <= 16)) {
-      e = launch_attend_stream(a, dtype, rows, true, false, behind, s);
-      if (e == cudaSuccess) e = launch_attend_stream(a, dtype, a.group, false, true, false, s);
-    } else {
-      e = launch_attend_stream(a, dtype, ss ? a.group : rows, sp, ss, behind, s);
-    }
+    e = launch_attend_stream(a, dtype, sp, ss, tp || ts, s);
     if (e != cudaSuccess) return e;
   }
   if (mla) {

@@ -76,8 +76,9 @@ struct AttendArgs {
   uint32_t tiles[2];                          // by kv_attend_tiles.cu ...
   uint32_t stream[2];                         // ... or by kv_attend_stream.cu
   // The tokens of a segment are worked on in chunks of chunk_tokens[kind], whose results are parts:
-  // part c of (sequence s, query head j) is at (s * q_heads + j) * n_parts + c, prefix chunks first.
-  uint32_t chunk_tokens[2], chunks[2], n_parts;
+  // part c of (sequence s, query head j) is at (s * q_heads + j) * n_parts + c, prefix chunks first; a chunk has
+  // per_chunk parts.
+  uint32_t chunk_tokens[2], chunks[2], per_chunk[2], n_parts;
   float* part_o;                              // [..][dv], normalised
   float* part_lse;                            // log2 of the part's sum of exponentials
   uint32_t direct;                            // one part: written to out and lse straight away
@@ -130,11 +131,11 @@ cudaError_t launch_attend(const AttendArgs& a, int dtype, bool mla, cudaStream_t
 bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows, bool weights);
 cudaError_t launch_attend_tiles(const AttendArgs& a, int dtype, bool mla, bool prefix, bool suffix, cudaStream_t s);
 
-// kv_attend_stream.cu: the same for up to 32 rows.  behind_tiles: launch_attend_tiles went ahead in this call, and the two
+// kv_attend_stream.cu: the same for up to 16 rows.  behind_tiles: launch_attend_tiles went ahead in this call, and the two
 // may run side by side.
 bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows);
-uint32_t stream_warps(uint32_t dk, uint32_t rows);   // of an SM
-cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, uint32_t rows, bool prefix, bool suffix, bool behind_tiles,
+uint32_t stream_warps(uint32_t dk);   // of an SM
+cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, bool prefix, bool suffix, bool behind_tiles,
                                  cudaStream_t s);
 
 // kv_append.cu

@@ -110,7 +110,7 @@ __device__ __forceinline__ void put_lse(const AttendArgs& a, uint32_t seq, uint3
 }
 
 __device__ __forceinline__ uint32_t part_of(const AttendArgs& a, const Item& w) {
-  return w.kind == kKindPrefix ? w.chunk : a.chunks[kKindPrefix] + w.chunk;
+  return w.kind == kKindPrefix ? w.chunk * a.per_chunk[0] : a.chunks[0] * a.per_chunk[0] + w.chunk * a.per_chunk[1];
 }
 
 // A sequence without tokens, where no join follows; by `threads` threads.

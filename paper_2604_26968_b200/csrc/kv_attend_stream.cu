@@ -3,9 +3,9 @@
 //
 // A warp takes a chunk of a segment in units of 16 tokens of one block; a block that is not in HBM is no unit.  It has a ring
 // of units of its own, filled by TMA (a box of 16 rows x 64 elements, swizzled, for each panel of K and V) which it issues
-// itself as it empties them: no warp waits for another.  A unit's scores (16 kM rows x 16 tokens) and output are mma.sync
+// itself as it empties them: no warp waits for another.  A unit's scores (16 rows x 16 tokens) and output are mma.sync
 // products whose operands come from the ring by ldmatrix, free of bank conflicts thanks to the swizzle.  The output is
-// rescaled only when a maximum has grown by more than 2^8.
+// rescaled only when a maximum has grown.
 // Bound: HBM.  A unit takes a warp about 2,000 cycles, most of them latencies of its short products and reductions, so it takes
 // eight to sixteen warps on every SM, each with two to three units under way; a chunk's start (its segment, its blocks' handles and
 // places, the first copies: five reads one after the other) costs as much as three units.
@@ -19,20 +19,20 @@ constexpr int kUnit = kStreamUnit;        // tokens
 constexpr int kStreamWarps = 4;
 constexpr uint32_t kMaxUnits = kStreamTokens / kUnit;
 
-template <int D, int kM>
+template <int D>
 struct Stream {
   static constexpr int kPanels = D / 64, kPanelBytes = kUnit * 128, kUnitBytes = 2 * kPanels * kPanelBytes;
-  static constexpr int kSlots = D == 64 || kM == 2 ? 3 : 2;
-  static constexpr int kCtas = D == 64 ? (kM == 2 ? 3 : 4) : (kM == 2 ? 2 : 3);   // of an SM
+  static constexpr int kSlots = D == 64 ? 3 : 2;
+  static constexpr int kCtas = D == 64 ? 4 : 3;   // of an SM
   static constexpr size_t kRing = (size_t)kStreamWarps * kSlots * kUnitBytes;
   static constexpr size_t kSmem = 1024 + kRing + kStreamWarps * (kMaxUnits * 8 + kSlots * 8 + 8);
 };
 
-template <typename T, int D, int kM, bool kWeights>
-__global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
+template <typename T, int D, bool kWeights>
+__global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
     stream_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, uint32_t first_kind_items, uint32_t items,
                   uint32_t behind_tiles) {
-  using S = Stream<D, kM>;
+  using S = Stream<D>;
   extern __shared__ uint8_t raw[];
   uint8_t* const smem = raw + ((1024u - (smem_address(raw) & 1023u)) & 1023u);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
   uint32_t item = blockIdx.x * kStreamWarps + warp;
   if (item >= items) return;
   const bool second = item >= first_kind_items;
-  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? item - first_kind_items : item, kM * 16, w, lane == 0)) return;
+  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? item - first_kind_items : item, 16, w, lane == 0)) return;
   if (w.to == 0) {
     put_nothing<T>(a, w, lane, 32);
     return;
@@ -100,36 +100,29 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
 #pragma unroll
   for (int k = 0; k < S::kSlots; ++k) issue(k, k);
   // queries straight into the operands' registers: rows lane / 4 and 8 further on, elements 2 (lane % 4) and 8 further on
-  uint32_t q[kM][D / 16][4];
+  uint32_t q[D / 16][4];
 #pragma unroll
-  for (int i = 0; i < kM; ++i)
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t r = lane / 4 + h * 8;
+    const bool there = r < w.rows;
+    uint32_t seq = 0, head = 0;
+    if (there) row_of(a, w, r, seq, head);
+    const uint16_t* const src = static_cast<const uint16_t*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + (lane & 3) * 2;
+    const bool words = (reinterpret_cast<uintptr_t>(src) & 3u) == 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t r = i * 16 + lane / 4 + h * 8;
-      const bool there = r < w.rows;
-      uint32_t seq = 0, head = 0;
-      if (there) row_of(a, w, r, seq, head);
-      const uint16_t* const src = static_cast<const uint16_t*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + (lane & 3) * 2;
-      const bool words = (reinterpret_cast<uintptr_t>(src) & 3u) == 0;
+    for (int k = 0; k < D / 16; ++k)
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint16_t* const x = src + k * 16 + e * 8;
-          q[i][k][h + 2 * e] = !there ? 0u : words ? *reinterpret_cast<const uint32_t*>(x) : (uint32_t)x[0] | (uint32_t)x[1] << 16;
-        }
-    }
-
-  float o[kM][D / 8][4], m[kM][2], l[kM][2];
-#pragma unroll
-  for (int i = 0; i < kM; ++i) {
-    m[i][0] = m[i][1] = -INFINITY;
-    l[i][0] = l[i][1] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
+      for (int e = 0; e < 2; ++e) {
+        const uint16_t* const x = src + k * 16 + e * 8;
+        q[k][h + 2 * e] = !there ? 0u : words ? *reinterpret_cast<const uint32_t*>(x) : (uint32_t)x[0] | (uint32_t)x[1] << 16;
+      }
   }
+
+  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
   const uint32_t k_row = (lane >> 4) * 8 + (lane & 7), v_row = (lane >> 3 & 1) * 8 + (lane & 7);
   uint32_t slot = 0, parity = 0;
   bool ok = true;
@@ -148,78 +141,69 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
       __syncwarp();
     }
     // scores, the even and the odd steps of the sum on their own
-    float s[kM][2][2][4];
+    float s[2][2][4];
 #pragma unroll
-    for (int i = 0; i < kM; ++i)
-#pragma unroll
-      for (int x = 0; x < 16; ++x) s[i][x / 8][x / 4 % 2][x % 4] = 0.0f;
+    for (int x = 0; x < 16; ++x) s[x / 8][x / 4 % 2][x % 4] = 0.0f;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       uint32_t b[4];
       const uint32_t c = 2 * k + (lane >> 3 & 1);
       ldmatrix4(b, k_at + c / 8 * S::kPanelBytes + (((c & 7) ^ (k_row & 7)) * 16));
+      mma<T>(s[k & 1][0], q[k], b[0], b[1]);
+      mma<T>(s[k & 1][1], q[k], b[2], b[3]);
+    }
+    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-      for (int i = 0; i < kM; ++i) {
-        mma<T>(s[i][k & 1][0], q[i][k], b[0], b[1]);
-        mma<T>(s[i][k & 1][1], q[i][k], b[2], b[3]);
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = (s[0][n][e] + s[1][n][e]) * a.scale2;
+        if (left < (uint32_t)kUnit && n * 8u + (lane & 3) * 2u + (e & 1) >= left) x = -INFINITY;
+        s[0][n][e] = x;
+        top[e >> 1] = fmaxf(top[e >> 1], x);
+      }
+    float turn[2] = {1.0f, 1.0f};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float mx = quad_max(top[h]);
+      if (mx > m[h]) {
+        turn[h] = exp2_(m[h] - mx);
+        m[h] = mx;
+        l[h] *= turn[h];
       }
     }
-    uint32_t p[kM][4];
+    if (__any_sync(~0u, turn[0] != 1.0f || turn[1] != 1.0f)) {
 #pragma unroll
-    for (int i = 0; i < kM; ++i) {
-      float top[2] = {-INFINITY, -INFINITY};
+      for (int d = 0; d < D / 8; ++d) {
+        o[d][0] *= turn[0];
+        o[d][1] *= turn[0];
+        o[d][2] *= turn[1];
+        o[d][3] *= turn[1];
+      }
+    }
+    const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+    float part[2] = {0.0f, 0.0f};
+    uint32_t p[4];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int n = 0; n < 2; ++n) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = (s[i][0][n][e] + s[i][1][n][e]) * a.scale2;
-          if (left < (uint32_t)kUnit && n * 8u + (lane & 3) * 2u + (e & 1) >= left) x = -INFINITY;
-          s[i][0][n][e] = x;
-          top[e >> 1] = fmaxf(top[e >> 1], x);
-        }
-      // the base follows the maximum when it has grown by 8 (or from nothing)
-      float turn[2] = {1.0f, 1.0f};
+      for (int e = 0; e < 4; ++e) {
+        const float x = exp2_(s[0][n][e] - base[e >> 1]);
+        s[0][n][e] = x;
+        part[e >> 1] += x;
+      }
+      p[2 * n] = pack2<T>(s[0][n][0], s[0][n][1]);
+      p[2 * n + 1] = pack2<T>(s[0][n][2], s[0][n][3]);
+    }
+    l[0] += part[0];
+    l[1] += part[1];
+    if (kWeights) {
+      float* const grain = grain_at(a, w, at / 16u);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float mx = quad_max(top[h]);
-        if (mx > m[i][h] + 8.0f || (m[i][h] == -INFINITY && mx > m[i][h])) {
-          turn[h] = exp2_(m[i][h] - mx);
-          m[i][h] = mx;
-          l[i][h] *= turn[h];
-        }
-      }
-      if (__any_sync(~0u, turn[0] != 1.0f || turn[1] != 1.0f)) {
-#pragma unroll
-        for (int d = 0; d < D / 8; ++d) {
-          o[i][d][0] *= turn[0];
-          o[i][d][1] *= turn[0];
-          o[i][d][2] *= turn[1];
-          o[i][d][3] *= turn[1];
-        }
-      }
-      const float base[2] = {m[i][0] == -INFINITY ? 0.0f : m[i][0], m[i][1] == -INFINITY ? 0.0f : m[i][1]};
-      float part[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = exp2_(s[i][0][n][e] - base[e >> 1]);
-          s[i][0][n][e] = x;
-          part[e >> 1] += x;
-        }
-        p[i][2 * n] = pack2<T>(s[i][0][n][0], s[i][0][n][1]);
-        p[i][2 * n + 1] = pack2<T>(s[i][0][n][2], s[i][0][n][3]);
-      }
-      l[i][0] += part[0];
-      l[i][1] += part[1];
-      if (kWeights) {
-        float* const grain = grain_at(a, w, at / 16u);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float sum = quad_sum(part[h]);
-          const uint32_t r = i * 16 + lane / 4 + h * 8;
-          if ((lane & 3) == 0 && r < w.rows) grain[r] = base[h] + log2_(sum);
-        }
+        const float sum = quad_sum(part[h]);
+        const uint32_t r = lane / 4 + h * 8;
+        if ((lane & 3) == 0 && r < w.rows) grain[r] = base[h] + log2_(sum);
       }
     }
 #pragma unroll
@@ -227,11 +211,8 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
       uint32_t b[4];
       const uint32_t c = 2 * d + (lane >> 4);
       ldmatrix4t(b, v_at + c / 8 * S::kPanelBytes + (((c & 7) ^ (v_row & 7)) * 16));
-#pragma unroll
-      for (int i = 0; i < kM; ++i) {
-        mma<T>(o[i][2 * d], p[i], b[0], b[1]);
-        mma<T>(o[i][2 * d + 1], p[i], b[2], b[3]);
-      }
+      mma<T>(o[2 * d], p, b[0], b[1]);
+      mma<T>(o[2 * d + 1], p, b[2], b[3]);
     }
     __syncwarp();
     issue(j + S::kSlots, slot);
@@ -246,19 +227,17 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D, kM>::kCtas)
   }
   const uint32_t part = part_of(a, w);
 #pragma unroll
-  for (int i = 0; i < kM; ++i)
+  for (int h = 0; h < 2; ++h) {
+    const float sum = quad_sum(l[h]);
+    const uint32_t r = lane / 4 + h * 8;
+    if (r >= w.rows) continue;
+    uint32_t seq, head;
+    row_of(a, w, r, seq, head);
+    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float sum = quad_sum(l[i][h]);
-      const uint32_t r = i * 16 + lane / 4 + h * 8;
-      if (r >= w.rows) continue;
-      uint32_t seq, head;
-      row_of(a, w, r, seq, head);
-      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j) put2<T>(a, seq, head, part, j * 8 + (lane & 3) * 2, o[i][j][2 * h] * inv, o[i][j][2 * h + 1] * inv);
-      if ((lane & 3) == 0) put_lse(a, seq, head, part, sum != 0.0f ? m[i][h] + log2_(sum) : -INFINITY);
-    }
+    for (int j = 0; j < D / 8; ++j) put2<T>(a, seq, head, part, j * 8 + (lane & 3) * 2, o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
+    if ((lane & 3) == 0) put_lse(a, seq, head, part, sum != 0.0f ? m[h] + log2_(sum) : -INFINITY);
+  }
 }
 
 typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -278,28 +257,22 @@ Encode encoder() {
   return f;
 }
 
-template <typename T, int D, int kM>
+template <typename T, int D>
 cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
-  using S = Stream<D, kM>;
+  using S = Stream<D>;
   const TableView& tv = a.tv;
   CUtensorMap map;
   if (!block_map(tv, D, kUnit, &map)) return cudaErrorInvalidValue;
-  const uint64_t rows = (uint64_t)a.max_members * a.group, tile = kM * 16;
+  const uint64_t rows = (uint64_t)a.max_members * a.group, tile = 16;
   const uint64_t np = prefix ? (rows + tile - 1) / tile * a.chunks[0] * tv.heads * a.n_groups : 0;
   const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
   if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
-  auto* kernel = a.weight ? stream_kernel<T, D, kM, true> : stream_kernel<T, D, kM, false>;
+  auto* kernel = a.weight ? stream_kernel<T, D, true> : stream_kernel<T, D, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
   return launch_overlapped_smem(kernel, (unsigned)((np + ns + kStreamWarps - 1) / kStreamWarps), (unsigned)kStreamWarps * 32, S::kSmem, s, a, map,
                                 (uint32_t)np, (uint32_t)(np + ns), behind_tiles ? 1u : 0u);
-}
-
-template <typename T>
-cudaError_t launch_typed(const AttendArgs& a, uint32_t rows, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
-  if (a.dk == 128) return rows <= 16 ? launch<T, 128, 1>(a, prefix, suffix, behind_tiles, s) : launch<T, 128, 2>(a, prefix, suffix, behind_tiles, s);
-  return rows <= 16 ? launch<T, 64, 1>(a, prefix, suffix, behind_tiles, s) : launch<T, 64, 2>(a, prefix, suffix, behind_tiles, s);
 }
 
 }  // namespace
@@ -318,13 +291,12 @@ bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uin
   return !mla && (dk == 128 || dk == 64) && block_tokens % kUnit == 0 && slab_rows < 0x7fff0000ull && has_block_map();
 }
 
-uint32_t stream_warps(uint32_t dk, uint32_t rows) {
-  return kStreamWarps * (dk == 64 ? (rows <= 16 ? Stream<64, 1>::kCtas : Stream<64, 2>::kCtas) : (rows <= 16 ? Stream<128, 1>::kCtas : Stream<128, 2>::kCtas));
-}
+uint32_t stream_warps(uint32_t dk) { return kStreamWarps * (dk == 64 ? Stream<64>::kCtas : Stream<128>::kCtas); }
 
-cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, uint32_t rows, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
-  return dtype == KV_DTYPE_BF16 ? launch_typed<__nv_bfloat16>(a, rows, prefix, suffix, behind_tiles, s)
-                                : launch_typed<__half>(a, rows, prefix, suffix, behind_tiles, s);
+cudaError_t launch_attend_stream(const AttendArgs& a, int dtype, bool prefix, bool suffix, bool behind_tiles, cudaStream_t s) {
+  if (dtype == KV_DTYPE_BF16)
+    return a.dk == 128 ? launch<__nv_bfloat16, 128>(a, prefix, suffix, behind_tiles, s) : launch<__nv_bfloat16, 64>(a, prefix, suffix, behind_tiles, s);
+  return a.dk == 128 ? launch<__half, 128>(a, prefix, suffix, behind_tiles, s) : launch<__half, 64>(a, prefix, suffix, behind_tiles, s);
 }
 
 }  // namespace kvt

@@ -125,7 +125,7 @@ struct Shape {
   static constexpr int kAPanels = kLatent ? (kDk - kCols) / 64 : kDk / 64, kBPanels = kCols / 64;
   static constexpr int kKBytes = kAPanels * kPanelBytes, kVBytes = kBPanels * kPanelBytes;
   static constexpr int kQBytes = kTiles * kQPanels * 128 * 128;
-  static constexpr int kMasks = kStages + 2;                // a mask is written again kStages + 2 tiles on, see the softmax
+  static constexpr int kMasks = 8;                          // see the softmax
   static constexpr int kFirst = kTiles == 2 ? 4 : 2;        // first warp of the softmax
   static constexpr int kThreads = (kFirst + 4 * kTiles) * 32;
   // tensor memory columns: outputs, then scores, then Q
@@ -152,20 +152,24 @@ __host__ __device__ constexpr int panel_at(int part, int p, int col0) {
   return !S::kLatent ? p * 64 : part ? col0 + p * 64 : p * 64 + (p * 64 >= col0 ? S::kCols : 0);
 }
 
-// The products of row tile r.  While the probabilities of tile t are formed, the scores of tile t + 1 are.
+// The products of team r.  While the probabilities of tile t are formed, the scores of tile t + 1 are.
 template <typename T, typename S, int kCol0>
-__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int r_, uint32_t n_tiles_, uint32_t* status) {
+__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int r_, uint32_t n_tiles_, bool shared_, uint32_t* status) {
   constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
   constexpr uint32_t kScores = instruction<T>(S::kTok, false), kOutput = instruction<T>(S::kCols, true);
   volatile uint32_t* const gave_up = &ctl->gave_up;
   // (the same for the whole warp, so that addresses and descriptors stay in uniform registers)
   const uint32_t tmem = __shfl_sync(~0u, tmem_, 0), n_tiles = __shfl_sync(~0u, n_tiles_, 0);
   const int r = __shfl_sync(~0u, r_, 0);
-  const uint32_t q_op = operand(q_at + r * (S::kQPanels * 16384), 0), o_at = tmem + r * S::kCols;
-  // S_r[t & 1] (+)= Q_r K_t^T over the elements of a stage's part
-  auto scores = [&](uint32_t t, int part) {
+  const bool shared = __shfl_sync(~0u, (int)shared_, 0) != 0;
+  const int q_tile = shared ? 0 : r;
+  const uint32_t q_op = operand(q_at + q_tile * (S::kQPanels * 16384), 0), o_at = tmem + r * S::kCols;
+  // (tiles counted by themselves: i; in the ring: t)
+  auto place = [&](uint32_t i) { return shared ? 2u * i + (uint32_t)r : i; };
+  // S_r[i & 1] (+)= Q_r K_t^T over the elements of a stage's part
+  auto scores = [&](uint32_t i, uint32_t t, int part) {
     const uint32_t k_op = operand(ring_at + (t % S::kStages) * kStage + (part ? S::kKBytes : 0), 0);
-    const uint32_t d = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok;
+    const uint32_t d = tmem + S::kSAt + (2 * r + (i & 1)) * S::kTok;
 #pragma unroll
     for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p) {
       const int at = panel_at<S>(part, p, kCol0);
@@ -177,52 +181,52 @@ __device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_a
       }
     }
   };
-  auto output = [&](uint32_t t) {   // O_r += P_r[t & 1] V_t
+  auto output = [&](uint32_t i, uint32_t t) {   // O_r += P_r[i & 1] V_t
     const uint32_t v_op = operand(ring_at + (t % S::kStages) * kStage + S::kKBytes, S::kPanelBytes);
-    const uint32_t p_at = tmem + S::kSAt + (2 * r + (t & 1)) * S::kTok;
+    const uint32_t p_at = tmem + S::kSAt + (2 * r + (i & 1)) * S::kTok;
 #pragma unroll
-    for (int k = 0; k < S::kTok / 16; ++k) mma_ts(o_at, p_at + k * 8, v_op + k * 128, kOutput, k ? 1u : t);
+    for (int k = 0; k < S::kTok / 16; ++k) mma_ts(o_at, p_at + k * 8, v_op + k * 128, kOutput, k ? 1u : i);
   };
   auto wait = [&](unsigned long long* bar, uint32_t parity) {
     return __all_sync(~0u, bar_wait(smem_address(bar), parity, gave_up, status));
   };
-  auto next_scores = [&](uint32_t t) {
-    const uint32_t st = t % S::kStages, parity = (t / S::kStages) & 1;
+  auto next_scores = [&](uint32_t i) {
+    const uint32_t t = place(i), st = t % S::kStages, parity = (t / S::kStages) & 1;
     if (!wait(&ctl->k_full[st], parity)) return false;
     // these scores take the place of probabilities that an output of two tiles ago is formed from: products of
     // different accumulators may overlap, so it has to be complete
-    if (t >= 2 && !wait(&ctl->pv_done[r], t & 1)) return false;
+    if (i >= 2 && !wait(&ctl->pv_done[r], i & 1)) return false;
     fence_after();
     if (elected()) {
-      scores(t, 0);
-      if (!S::kLatent) commit(smem_address(&ctl->s_full[2 * r + (t & 1)]));
+      scores(i, t, 0);
+      if (!S::kLatent) commit(smem_address(&ctl->s_full[2 * r + (i & 1)]));
       commit(smem_address(&ctl->k_empty[st]));
     }
     __syncwarp();
     if (S::kLatent) {
       if (!wait(&ctl->v_full[st], parity)) return false;
       if (elected()) {
-        scores(t, 1);
-        commit(smem_address(&ctl->s_full[t & 1]));
+        scores(i, t, 1);
+        commit(smem_address(&ctl->s_full[i & 1]));
       }
       __syncwarp();
     }
     return true;
   };
-  if (!wait(&ctl->q_ready[r], 0)) return;
+  if (!wait(&ctl->q_ready[q_tile], 0)) return;
   fence_after();
   if (!next_scores(0)) return;
-  for (uint32_t t = 0; t < n_tiles; ++t) {
-    if (t + 1 < n_tiles && !next_scores(t + 1)) return;
-    const uint32_t st = t % S::kStages;
+  for (uint32_t i = 0; i < n_tiles; ++i) {
+    if (i + 1 < n_tiles && !next_scores(i + 1)) return;
+    const uint32_t t = place(i), st = t % S::kStages;
     if (!S::kLatent && !wait(&ctl->v_full[st], (t / S::kStages) & 1)) return;
-    if (!wait(&ctl->p_ready[2 * r + (t & 1)], (t >> 1) & 1)) return;
+    if (!wait(&ctl->p_ready[2 * r + (i & 1)], (i >> 1) & 1)) return;
     fence_after();
     if (elected()) {
-      output(t);
+      output(i, t);
       commit(smem_address(&ctl->pv_done[r]));
       commit(smem_address(&ctl->v_empty[st]));
-      if (t + 1 == n_tiles) commit(smem_address(&ctl->o_done[r]));
+      if (i + 1 == n_tiles) commit(smem_address(&ctl->o_done[r]));
     }
     __syncwarp();
   }
@@ -302,16 +306,19 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     if (col0 == 0) put_nothing<T>(a, w, threadIdx.x, blockDim.x);
     return;
   }
-  const int row_tiles = w.rows > 128u ? 2 : 1;
+  // Two teams, each with its scores, output and softmax: of a row tile each, or, where one is all there can be, of every
+  // other tile of tokens (their results are parts of their own).
+  const bool shared = a.per_chunk[w.kind] == 2u;
+  const int teams = shared || w.rows > 128u ? 2 : 1;
   const TableView& tv = a.tv;
   const uint32_t n_tiles = (w.to - w.from + S::kTok - 1u) / S::kTok;
 
   if (threadIdx.x == 0) {
     for (int b = 0; b < 4; ++b) {
       bar_init(smem_address(&ctl->k_full[b]), 1);
-      bar_init(smem_address(&ctl->k_empty[b]), row_tiles);
+      bar_init(smem_address(&ctl->k_empty[b]), shared ? 1 : teams);
       bar_init(smem_address(&ctl->v_full[b]), 1);
-      bar_init(smem_address(&ctl->v_empty[b]), row_tiles);
+      bar_init(smem_address(&ctl->v_empty[b]), shared ? 1 : teams);
       bar_init(smem_address(&ctl->s_full[b]), 1);
       bar_init(smem_address(&ctl->p_ready[b]), 128);
     }
@@ -390,29 +397,40 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     // ---- matrix instructions: a warp for each row tile; the whole warp waits, one thread issues ----
     if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int r = warp - 1;
-    if (r < row_tiles) {
-      if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, n_tiles, status);
-      else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, n_tiles, status);
+    const uint32_t mine = shared ? (n_tiles + 1u - r) / 2u : n_tiles;
+    if (r < teams && mine) {
+      if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, status);
+      else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, status);
     }
   } else {
     // ---- softmax: a thread per row ----
     if (S::kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");   // 128 x (72 + 2 x 216) of 384 x 168
     const int r = (warp - S::kFirst) / 4;
     const uint32_t lane_at = (uint32_t)(warp & 3) * 32u;   // a warp reaches the lanes of its number modulo four
-    const uint32_t row = r * 128u + lane_at + lane;
-    if (r < row_tiles) {
+    const uint32_t row = (shared ? 0u : r * 128u) + lane_at + lane;
+    const uint32_t my_tiles = shared ? (n_tiles + 1u - r) / 2u : n_tiles;
+    if (r < teams && !my_tiles) {
+      if (row < w.rows) {     // (a chunk of one tile: nothing for the second team)
+        uint32_t seq, head;
+        row_of(a, w, row, seq, head);
+        put_lse(a, seq, head, part_of(a, w) + r, -INFINITY);
+      }
+    } else if (r < teams) {
       const bool mine = row < w.rows;
       const uint32_t o_at = tmem + (lane_at << 16) + r * S::kCols;
-      load_queries<T, S>(a, w, q_s, tmem, r, threadIdx.x - (S::kFirst + 4 * r) * 32, lane_at, q_sign, q_bits);
-      bar_arrive(smem_address(&ctl->q_ready[r]));
+      if (r == 0 || !shared) {
+        load_queries<T, S>(a, w, q_s, tmem, r, threadIdx.x - (S::kFirst + 4 * r) * 32, lane_at, q_sign, q_bits);
+        bar_arrive(smem_address(&ctl->q_ready[r]));
+      }
       float m = -INFINITY, l = 0.0f;
       bool ok = true;
-      for (uint32_t t = 0; t < n_tiles; ++t) {
-        const int slot = 2 * r + (int)(t & 1);
+      for (uint32_t i = 0; i < my_tiles; ++i) {
+        const uint32_t t = shared ? 2u * i + r : i;
+        const int slot = 2 * r + (int)(i & 1);
         const uint32_t s_at = tmem + (lane_at << 16) + S::kSAt + slot * S::kTok;
-        // (the tile's mask was written ahead of the copies that the scores have waited for, and is not written
-        // again before scores that wait for this tile's output are complete)
-        ok = bar_wait(smem_address(&ctl->s_full[slot]), (t >> 1) & 1, gave_up, status);
+        // (The tile's mask was written ahead of the copies that the scores have waited for.  It is written again eight tiles on,
+        // when the scores four tiles on are complete, which have waited for this tile's output.)
+        ok = bar_wait(smem_address(&ctl->s_full[slot]), (i >> 1) & 1, gave_up, status);
         ok = __all_sync(~0u, ok);
         if (!ok) break;
         fence_after();
@@ -452,9 +470,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         }
         const float base = m == -INFINITY ? 0.0f : m;
         const Pair scale(a.scale2, a.scale2), minus(-base, -base);
-        if (t > 0 && __any_sync(~0u, turn_by != 1.0f)) {
+        if (i > 0 && __any_sync(~0u, turn_by != 1.0f)) {
           // (no product of this row tile is under way: the next waits for these probabilities)
-          ok = bar_wait(smem_address(&ctl->pv_done[r]), (t - 1) & 1, gave_up, status);
+          ok = bar_wait(smem_address(&ctl->pv_done[r]), (i - 1) & 1, gave_up, status);
           ok = __all_sync(~0u, ok);
           if (!ok) break;
           fence_after();
@@ -514,7 +532,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         fence_after();
         uint32_t seq = 0, head = 0;
         if (mine) row_of(a, w, row, seq, head);
-        const uint32_t part = part_of(a, w);
+        const uint32_t part = part_of(a, w) + (shared ? r : 0);
         const float inv = l != 0.0f ? 1.0f / l : 0.0f;
 #pragma unroll 1
         for (int c = 0; c < S::kCols / 32; ++c) {

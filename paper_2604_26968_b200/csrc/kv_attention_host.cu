@@ -47,10 +47,10 @@ TableView table_view(const PoolView& v, int32_t q, int32_t layer, const uint32_t
 // How a call's work is split: tokens of a chunk and chunks, for prefixes and suffixes.
 constexpr uint32_t kSms = 148;
 // Rows from which on a segment goes to the tensor cores' 128-row tiles.
-constexpr uint32_t kTileRows = 33;
+constexpr uint32_t kTileRows = 17;
 struct Split {
   bool tiles[2], stream[2];
-  uint32_t chunk_tokens[2], chunks[2], n_parts, grain_tokens, grains[2];
+  uint32_t chunk_tokens[2], chunks[2], per_chunk[2], n_parts, grain_tokens, grains[2];
   uint64_t lse_at, grain_at[2], bytes;
 };
 
@@ -88,6 +88,7 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
   out->tiles[0] = out->tiles[1] = out->stream[0] = out->stream[1] = false;
   out->chunk_tokens[0] = out->chunk_tokens[1] = 64;
   out->chunks[0] = out->chunks[1] = 0;
+  out->per_chunk[0] = out->per_chunk[1] = 1;
   const uint64_t prefix_rows = (uint64_t)max_members * group;
   const uint64_t slab_rows = v.geom[q].n * v.geom[q].n_chunks * bt;
   const bool streams = stream_takes(dk, dv, mla, bt, slab_rows);
@@ -100,20 +101,20 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
     uint64_t limit = (uint64_t)kMaxChunkBlocks * bt / 64 * 64;   // most tokens of a chunk
     if (limit < 64) limit = 64;
     if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
-    out->stream[k] = !out->tiles[k] && streams && rows <= 32;
+    out->stream[k] = !out->tiles[k] && streams && rows <= 16;
     if (out->tiles[k]) {
       const uint64_t tile = mla ? 128 : 256;
+      out->per_chunk[k] = !mla && rows <= 128 ? 2 : 1;
       split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
     } else if (out->stream[k]) {
-      const uint64_t tile = rows <= 16 ? 16 : 32;
-      split_segment((rows + tile - 1) / tile * segs, most, kStreamUnit, kSms * stream_warps(dk, (uint32_t)rows), 3, kStreamTokens, !shared, &out->chunk_tokens[k],
+      split_segment(segs, most, kStreamUnit, kSms * stream_warps(dk), 3, kStreamTokens, !shared, &out->chunk_tokens[k],
                     &out->chunks[k]);
     } else {
       const uint64_t tile = mla ? 64 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
       split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
     }
   }
-  out->n_parts = out->chunks[0] + out->chunks[1];
+  out->n_parts = out->chunks[0] * out->per_chunk[0] + out->chunks[1] * out->per_chunk[1];
   out->grain_tokens = bt % 16 == 0 ? 16 : 1;
   const unsigned __int128 rows = (unsigned __int128)n_seqs * q_heads;
   unsigned __int128 at = 0;
@@ -200,6 +201,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
     a.stream[k] = sp.stream[k];
     a.chunk_tokens[k] = sp.chunk_tokens[k];
     a.chunks[k] = sp.chunks[k];
+    a.per_chunk[k] = sp.per_chunk[k];
     a.grains[k] = sp.grains[k];
     a.grain[k] = reinterpret_cast<float*>(scratch + sp.grain_at[k]);
   }

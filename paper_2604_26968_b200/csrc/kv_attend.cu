@@ -7,7 +7,7 @@
 // KV head -- of all members of a group, where it is a prefix -- are the rows of one small matrix product
 // per block, so that a block's K and V leave HBM once for all of them.  A segment's tokens are cut into
 // chunks that different CTAs work on; a part (one row, one chunk) is its normalised output and the log2 of
-// its sum of exponentials, and finish_kernel adds the parts up with weights 2^(lse_part - lse).
+// its sum of exponentials, and finish_kernel adds them up with weights 2^(lse_part - lse).
 #include "kv_attend_device.cuh"
 
 namespace kvt {
@@ -468,7 +468,6 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
 // ---- parts to outputs, grains to weights -------------------------------------------------------------
 
 constexpr int kFinishThreads = 256, kFinishRows = kFinishThreads / 32;
-constexpr uint32_t kWeightBlocks = 64, kWeightRows = 1024;   // blocks of a CTA, rows whose sums it holds at a time
 
 // The parts of a sequence: np of its group's prefix, ns of its suffix, the latter behind the places of all prefix chunks.
 struct Parts {
@@ -497,10 +496,14 @@ __device__ __forceinline__ uint32_t group_of_warp(const AttendArgs& a, uint32_t 
 template <typename T>
 __device__ __forceinline__ void join_rows(const AttendArgs& a, uint64_t row) {
   const uint32_t lane = threadIdx.x % 32;
-  if (row >= (uint64_t)a.n_seqs * a.q_heads) return;
+  if (row >= (uint64_t)a.n_seqs * a.q_heads) {
+    wait_for_kernel_ahead();
+    return;
+  }
   const uint32_t seq = (uint32_t)(row / a.q_heads), head = (uint32_t)(row - (uint64_t)seq * a.q_heads);
   const Parts parts = parts_of(a, seq, group_of_warp(a, seq));
   const uint32_t n = parts.np + parts.ns;
+  wait_for_kernel_ahead();      // (what is read above was there before the call's first kernel began)
   const float* const lse = a.part_lse + row * a.n_parts;
   const float first = lane < n ? lse[parts.place(lane)] : -INFINITY;
   float top = first;
@@ -513,7 +516,11 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, uint64_t row) {
 #pragma unroll
   for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(~0u, sum, d);
   const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-  if (lane == 0 && a.lse) a.lse[row] = sum != 0.0f ? (base + log2_(sum)) * 0.69314718055994530942f : -INFINITY;
+  if (lane == 0) {
+    const float total = sum != 0.0f ? base + log2_(sum) : -INFINITY;
+    if (a.lse) a.lse[row] = total * 0.69314718055994530942f;
+    if (a.weight) a.total[row] = total;
+  }
   T* const out = static_cast<T*>(a.out) + (int64_t)seq * a.out_seq + (int64_t)head * a.out_head;
   const bool wide = (reinterpret_cast<uintptr_t>(out) & 7u) == 0;
   for (uint32_t d0 = 0; d0 < a.dv; d0 += 128u) {      // four neighbouring elements a lane
@@ -554,84 +561,66 @@ __device__ __forceinline__ void join_rows(const AttendArgs& a, uint64_t row) {
   }
 }
 
-// Weight of up to kWeightBlocks blocks of a segment and KV head: the sum over its rows of what the kernels have left for
-// their grains, taken from the rows' own sums.  `lanes` threads a block.
-__device__ __forceinline__ void add_weights(const AttendArgs& a, int kind, uint32_t item, uint32_t lanes, float* total) {
-  const uint32_t most_blocks = ((kind == kKindPrefix ? a.max_prefix : a.max_suffix) + a.tv.block_tokens - 1u) / a.tv.block_tokens;
-  const uint32_t spans = (most_blocks + kWeightBlocks - 1u) / kWeightBlocks;
-  const uint32_t block0 = item % spans * kWeightBlocks;
-  item /= spans;
-  const uint32_t head = item % a.tv.heads, index = item / a.tv.heads;
-  uint32_t seq0 = index, rows = a.group, stride = a.group;
-  Segment seg;
-  if (kind == kKindPrefix) {
-    uint32_t lo, hi;
-    a.members(index, lo, hi, false);
-    seq0 = lo;
-    rows = (hi - lo) * a.group;
-    stride = a.max_members * a.group;
-    seg = a.checked(a.prefix, index, a.max_prefix, false);
-  } else {
-    seg = a.checked(a.suffix, index, a.max_suffix, false);
-  }
-  if (block0 * a.tv.block_tokens >= seg.tokens) return;
-  const uint32_t group = threadIdx.x / lanes, lane = threadIdx.x % lanes, groups = kFinishThreads / lanes;
-  const uint32_t blocks = min(kWeightBlocks, (seg.tokens - 1u) / a.tv.block_tokens + 1u - block0);
-  const float* const grain = a.grain[kind] + ((uint64_t)index * a.tv.heads + head) * a.grains[kind] * stride;
-  for (uint32_t r0 = 0; r0 < rows; r0 += kWeightRows) {
-    const uint32_t here = min(kWeightRows, rows - r0);
-    __syncthreads();
-    for (uint32_t r = threadIdx.x; r < here; r += kFinishThreads) {
-      const uint32_t member = (r0 + r) / a.group, seq = seq0 + member;
-      const uint64_t row = (uint64_t)seq * a.q_heads + head * a.group + (r0 + r - member * a.group);
-      const float* const lse = a.part_lse + row * a.n_parts;
-      if (a.direct) {
-        total[r] = lse[0];
-        continue;
-      }
-      const Parts parts = parts_of(a, seq, kind == kKindPrefix ? index : a.n_groups ? a.group_of(seq) : ~0u);
-      float top = -INFINITY, sum = 0.0f;
-      for (uint32_t i = 0; i < parts.np + parts.ns; ++i) top = fmaxf(top, lse[parts.place(i)]);
-      const float base = top == -INFINITY ? 0.0f : top;
-      for (uint32_t i = 0; i < parts.np + parts.ns; ++i) sum += exp2_(lse[parts.place(i)] - base);
-      total[r] = base + log2_(sum);      // (-inf: no parts, or empty ones)
-    }
-    __syncthreads();
-    for (uint32_t b0 = 0; b0 < blocks; b0 += groups) {
-      const uint32_t b = block0 + b0 + group;
-      const uint64_t at = (uint64_t)seg.row + b;
-      unsigned long long w = 0;
-      uint32_t handle = KV_NONE;
-      if (b0 + group < blocks && a.tv.chunk(at, head) != ~0u) {
-        handle = a.tv.table[(at * a.tv.layers + a.tv.layer) * a.tv.heads + head];
-        const uint32_t from = b * a.tv.block_tokens, to = min(seg.tokens, from + a.tv.block_tokens);
-        const uint32_t g0 = from / a.grain_tokens, g1 = (to + a.grain_tokens - 1u) / a.grain_tokens;
-        float sum = 0.0f;
-        for (uint32_t r = lane; r < here; r += lanes) {
-          const float lse = total[r];
-          if (lse == -INFINITY) continue;
-          for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r0 + r] - lse);
-        }
-        // in units of 2^-32; NaN counts as nothing
-        const float x = sum * 0x1p32f;
-        w = x > 0.0f ? __float2ull_rn(fminf(x, 0x1p62f)) : 0ull;
-      }
-      for (uint32_t d = lanes / 2u; d; d /= 2u) w += __shfl_xor_sync(~0u, w, d);
-      if (lane == 0 && w) atomicAdd(a.weight + handle, w);
-    }
-  }
+template <typename T>
+__global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ AttendArgs a) {
+  join_rows<T>(a, (uint64_t)blockIdx.x * kFinishRows + threadIdx.x / 32);
 }
 
-// CTAs: rows to join, then spans of prefixes, then spans of suffixes.
-template <typename T>
-__global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_constant__ AttendArgs a, uint32_t join_ctas, uint32_t prefix_ctas,
-                                                                uint32_t prefix_lanes, uint32_t suffix_lanes) {
-  __shared__ float total[kWeightRows];
-  wait_for_kernel_ahead();
-  const uint32_t i = blockIdx.x;
-  if (i < join_ctas) join_rows<T>(a, (uint64_t)i * kFinishRows + threadIdx.x / 32);
-  else if (i < join_ctas + prefix_ctas) add_weights(a, kKindPrefix, i - join_ctas, prefix_lanes, total);
-  else add_weights(a, kKindSuffix, i - join_ctas - prefix_ctas, suffix_lanes, total);
+// Weight of the blocks of prefixes (the first prefix_blocks items) and suffixes: the sum over a block's rows of what the kernels have
+// left for its grains, taken from the rows' sums; `lanes` threads a block.
+__global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_constant__ AttendArgs a, uint32_t prefix_ctas, uint32_t prefix_lanes,
+                                                               uint32_t suffix_lanes) {
+  const int kind = blockIdx.x < prefix_ctas ? kKindPrefix : kKindSuffix;
+  const uint32_t lanes = kind == kKindPrefix ? prefix_lanes : suffix_lanes;
+  const uint64_t item = ((uint64_t)(blockIdx.x - (kind == kKindPrefix ? 0u : prefix_ctas)) * kFinishThreads + threadIdx.x) / lanes;
+  const uint32_t lane = threadIdx.x % lanes;
+  const uint32_t most_blocks = ((kind == kKindPrefix ? a.max_prefix : a.max_suffix) + a.tv.block_tokens - 1u) / a.tv.block_tokens;
+  const uint64_t sh = item / most_blocks;
+  const uint32_t b = (uint32_t)(item - sh * most_blocks);
+  const uint64_t index = sh / a.tv.heads;
+  const uint32_t head = (uint32_t)(sh - index * a.tv.heads);
+  unsigned long long w = 0;
+  uint32_t handle = KV_NONE;
+  if (index < (kind == kKindPrefix ? a.n_groups : a.n_seqs)) {
+    uint32_t seq0 = (uint32_t)index, rows = a.group, stride = a.group;
+    Segment seg;
+    if (kind == kKindPrefix) {
+      uint32_t lo, hi;
+      a.members((uint32_t)index, lo, hi, false);
+      seq0 = lo;
+      rows = (hi - lo) * a.group;
+      stride = a.max_members * a.group;
+      seg = a.checked(a.prefix, (uint32_t)index, a.max_prefix, false);
+    } else {
+      seg = a.checked(a.suffix, (uint32_t)index, a.max_suffix, false);
+    }
+    const uint32_t from = b * a.tv.block_tokens;
+    const uint64_t at = (uint64_t)seg.row + b;
+    const bool there = from < seg.tokens && rows && a.tv.chunk(at, head) != ~0u;
+    if (there) handle = a.tv.table[(at * a.tv.layers + a.tv.layer) * a.tv.heads + head];
+    wait_for_kernel_ahead();      // (what is read above was there before the call's first kernel began)
+    if (there) {
+      const uint32_t to = min(seg.tokens, from + a.tv.block_tokens);
+      const uint32_t g0 = from / a.grain_tokens, g1 = (to + a.grain_tokens - 1u) / a.grain_tokens;
+      const float* const total = a.direct ? a.part_lse : a.total;
+      const float* const grain = a.grain[kind] + (index * a.tv.heads + head) * (uint64_t)a.grains[kind] * stride;
+      float sum = 0.0f;
+#pragma unroll 4
+      for (uint32_t r = lane; r < rows; r += lanes) {
+        const uint32_t member = r / a.group;
+        const float lse = total[(uint64_t)(seq0 + member) * a.q_heads + head * a.group + (r - member * a.group)];
+        if (lse == -INFINITY) continue;
+        for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r] - lse);
+      }
+      // in units of 2^-32; NaN counts as nothing
+      const float x = sum * 0x1p32f;
+      w = x > 0.0f ? __float2ull_rn(fminf(x, 0x1p62f)) : 0ull;
+    }
+  } else {
+    wait_for_kernel_ahead();
+  }
+  for (uint32_t d = lanes / 2u; d; d /= 2u) w += __shfl_xor_sync(~0u, w, d);
+  if (lane == 0 && w) atomicAdd(a.weight + handle, w);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------
@@ -696,22 +685,24 @@ cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t 
   }
   if (e != cudaSuccess) return e;
   const uint64_t rows = (uint64_t)a.n_seqs * a.q_heads;
-  const uint64_t join = a.direct ? 0 : (rows + kFinishRows - 1) / kFinishRows;
-  uint64_t spans[2] = {0, 0};
-  uint32_t lanes[2] = {1, 1};
-  if (a.weight) {
-    for (int kind = prefix ? 0 : 1; kind < 2; ++kind) {
-      const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
-      const uint64_t blocks = ((uint64_t)most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
-      spans[kind] = (uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * ((blocks + kWeightBlocks - 1) / kWeightBlocks);
-      const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
-      while (lanes[kind] < 32u && lanes[kind] < r) lanes[kind] *= 2u;
-    }
+  const uint64_t join = (rows + kFinishRows - 1) / kFinishRows;
+  if (!a.direct) {
+    e = launch_overlapped(finish_kernel<T>, (unsigned)join, (unsigned)kFinishThreads, s, a);
+    if (e != cudaSuccess) return e;
   }
-  const uint64_t grid = join + spans[0] + spans[1];
-  if (!grid) return cudaSuccess;
-  if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
-  return launch_overlapped(finish_kernel<T>, (unsigned)grid, (unsigned)kFinishThreads, s, a, (uint32_t)join, (uint32_t)spans[0], lanes[0], lanes[1]);
+  if (!a.weight) return cudaSuccess;
+  uint64_t ctas[2] = {0, 0};
+  uint32_t lanes[2] = {1, 1};
+  for (int kind = prefix ? 0 : 1; kind < 2; ++kind) {
+    const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
+    const uint64_t blocks = ((uint64_t)most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
+    const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
+    while (lanes[kind] < 32u && lanes[kind] < r) lanes[kind] *= 2u;
+    ctas[kind] = ((uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks * lanes[kind] + kFinishThreads - 1) / kFinishThreads;
+  }
+  if (ctas[0] + ctas[1] == 0) return cudaSuccess;
+  if (ctas[0] + ctas[1] > 0x7fffffffull) return cudaErrorInvalidValue;
+  return launch_overlapped(weight_kernel, (unsigned)(ctas[0] + ctas[1]), (unsigned)kFinishThreads, s, a, (uint32_t)ctas[0], lanes[0], lanes[1]);
 }
 
 }  // namespace

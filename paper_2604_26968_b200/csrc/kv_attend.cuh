@@ -81,6 +81,7 @@ struct AttendArgs {
   uint32_t chunk_tokens[2], chunks[2], per_chunk[2], n_parts;
   float* part_o;                              // [..][dv], normalised
   float* part_lse;                            // log2 of the part's sum of exponentials
+  float* total;                               // the same of each row, where weights are asked for
   uint32_t direct;                            // one part: written to out and lse straight away
   // Attention weight of each `grain` tokens (log2 of the sum of exponentials), for every row:
   // prefix [group][head][grain][max_members * group], suffix [seq][head][grain][group].

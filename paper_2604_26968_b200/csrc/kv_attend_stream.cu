@@ -1,7 +1,7 @@
 // kv_attend where few rows read a block: a stream of blocks through independent warps (and the encoder of the maps
 // by which the kernels here and in kv_attend_tiles.cu copy blocks).
 //
-// A warp takes a chunk of a segment in units of 16 tokens of one block; a block that is not in HBM is no unit.  It has a ring
+// A warp takes chunks of segments, one after the other, in units of 16 tokens of one block; a block that is not in HBM is no unit.  It has a ring
 // of units of its own, filled by TMA (a box of 16 rows x 64 elements, swizzled, for each panel of K and V) which it issues
 // itself as it empties them: no warp waits for another.  A unit's scores (16 rows x 16 tokens) and output are mma.sync
 // products whose operands come from the ring by ldmatrix, free of bank conflicts thanks to the swizzle.  The output is
@@ -51,15 +51,6 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
     }
   } at_end{behind_tiles};
 
-  Item w;
-  uint32_t item = blockIdx.x * kStreamWarps + warp;
-  if (item >= items) return;
-  const bool second = item >= first_kind_items;
-  if (!item_of(a, second ? kKindSuffix : kKindPrefix, second ? item - first_kind_items : item, 16, w, lane == 0)) return;
-  if (w.to == 0) {
-    put_nothing<T>(a, w, lane, 32);
-    return;
-  }
   const TableView& tv = a.tv;
   if (lane == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&map) : "memory");
@@ -69,174 +60,190 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  uint32_t n_units = 0;
-  {
-    const uint32_t n = (w.to - w.from + kUnit - 1u) / kUnit;
-    uint32_t ch[kMaxUnits / 32];
-#pragma unroll
-    for (int k = 0; k < (int)kMaxUnits / 32; ++k) {
-      const uint32_t u = k * 32u + lane;
-      ch[k] = u < n ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(w.from + u * kUnit), w.head) : ~0u;
-    }
-#pragma unroll
-    for (int k = 0; k < (int)kMaxUnits / 32; ++k) {
-      const uint32_t at = w.from + (k * 32u + lane) * kUnit;
-      const uint32_t there = __ballot_sync(~0u, ch[k] != ~0u);
-      if (ch[k] != ~0u)
-        units[n_units + __popc(there & ((1u << lane) - 1u))] = make_uint2(ch[k] * tv.block_tokens + (at - tv.by_tokens(at) * tv.block_tokens), at);
-      n_units += __popc(there);
-    }
-  }
   __syncwarp();
-  // unit j into a slot, a lane for each box: panels of K, then of V
-  const int32_t box_x = (lane % S::kPanels) * 64, box_y = lane / S::kPanels ? (int32_t)(tv.heads * tv.block_tokens) : 0;
-  auto issue = [&](uint32_t j, uint32_t slot) {
-    if (j >= n_units) return;
-    const uint32_t b = smem_address(bar + slot);
-    if (lane == 0) bar_expect(b, S::kUnitBytes);
-    __syncwarp();
-    if (lane < 2 * S::kPanels) tma_box(smem_address(ring + slot * S::kUnitBytes + lane * S::kPanelBytes), &map, box_x, (int32_t)units[j].x + box_y, b);
-  };
-#pragma unroll
-  for (int k = 0; k < S::kSlots; ++k) issue(k, k);
-  // queries straight into the operands' registers: rows lane / 4 and 8 further on, elements 2 (lane % 4) and 8 further on
-  uint32_t q[D / 16][4];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const uint32_t r = lane / 4 + h * 8;
-    const bool there = r < w.rows;
-    uint32_t seq = 0, head = 0;
-    if (there) row_of(a, w, r, seq, head);
-    const uint16_t* const src = static_cast<const uint16_t*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + (lane & 3) * 2;
-    const bool words = (reinterpret_cast<uintptr_t>(src) & 3u) == 0;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint16_t* const x = src + k * 16 + e * 8;
-        q[k][h + 2 * e] = !there ? 0u : words ? *reinterpret_cast<const uint32_t*>(x) : (uint32_t)x[0] | (uint32_t)x[1] << 16;
-      }
-  }
-
-  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-#pragma unroll
-  for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+  // lanes' places in the ring's operands: rows of a unit's panels, 16-byte chunks exchanged by the row
   const uint32_t k_row = (lane >> 4) * 8 + (lane & 7), v_row = (lane >> 3 & 1) * 8 + (lane & 7);
+  uint32_t k_off[4], v_off[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    k_off[c] = smem_address(ring) + k_row * 128 + (((2 * c + (lane >> 3 & 1)) ^ (k_row & 7)) * 16);
+    v_off[c] = smem_address(ring) + S::kPanels * S::kPanelBytes + v_row * 128 + (((2 * c + (lane >> 4)) ^ (v_row & 7)) * 16);
+  }
+  const int32_t box_x = (lane % S::kPanels) * 64, box_y = lane / S::kPanels ? (int32_t)(tv.heads * tv.block_tokens) : 0;
   uint32_t slot = 0, parity = 0;
   bool ok = true;
-  for (uint32_t j = 0; j < n_units; ++j) {
-    ok = __all_sync(~0u, bar_wait(smem_address(bar + slot), parity, gave_up, tv.status));
-    if (!ok) break;
-    uint8_t* const unit = ring + slot * S::kUnitBytes;
-    const uint32_t k_at = smem_address(unit) + k_row * 128, v_at = smem_address(unit) + S::kPanels * S::kPanelBytes + v_row * 128;
-    const uint32_t at = units[j].y, left = w.to - at;
-    if (left < (uint32_t)kUnit) {
-      // what lies behind the last token would meet probabilities of zero: it may be anything
-      for (uint32_t x = lane; x < (kUnit - left) * S::kPanels * 8u; x += 32u) {
-        const uint32_t tok = left + x / (S::kPanels * 8u), c = x % (S::kPanels * 8u);
-        *reinterpret_cast<uint4*>(unit + (S::kPanels + c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
-      }
-      __syncwarp();
+  for (uint32_t item = blockIdx.x * kStreamWarps + warp; item < items && ok; item += gridDim.x * kStreamWarps) {
+    Item w;
+    const bool second = item >= first_kind_items;
+    if (!item_of<true>(a, second ? kKindSuffix : kKindPrefix, second ? item - first_kind_items : item, 16, w, lane == 0)) continue;
+    if (w.to == 0) {
+      put_nothing<T>(a, w, lane, 32);
+      continue;
     }
-    // scores, the even and the odd steps of the sum on their own
-    float s[2][2][4];
+    uint32_t n_units = 0;
+    {
+      const uint32_t n = (w.to - w.from + kUnit - 1u) / kUnit;
+      uint32_t ch[kMaxUnits / 32];
 #pragma unroll
-    for (int x = 0; x < 16; ++x) s[x / 8][x / 4 % 2][x % 4] = 0.0f;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      uint32_t b[4];
-      const uint32_t c = 2 * k + (lane >> 3 & 1);
-      ldmatrix4(b, k_at + c / 8 * S::kPanelBytes + (((c & 7) ^ (k_row & 7)) * 16));
-      mma<T>(s[k & 1][0], q[k], b[0], b[1]);
-      mma<T>(s[k & 1][1], q[k], b[2], b[3]);
-    }
-    float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float x = (s[0][n][e] + s[1][n][e]) * a.scale2;
-        if (left < (uint32_t)kUnit && n * 8u + (lane & 3) * 2u + (e & 1) >= left) x = -INFINITY;
-        s[0][n][e] = x;
-        top[e >> 1] = fmaxf(top[e >> 1], x);
+      for (int k = 0; k < (int)kMaxUnits / 32; ++k) {
+        const uint32_t u = k * 32u + lane;
+        ch[k] = u < n ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(w.from + u * kUnit), w.head) : ~0u;
       }
-    float turn[2] = {1.0f, 1.0f};
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float mx = quad_max(top[h]);
-      if (mx > m[h]) {
-        turn[h] = exp2_(m[h] - mx);
-        m[h] = mx;
-        l[h] *= turn[h];
+      for (int k = 0; k < (int)kMaxUnits / 32; ++k) {
+        const uint32_t at = w.from + (k * 32u + lane) * kUnit;
+        const uint32_t there = __ballot_sync(~0u, ch[k] != ~0u);
+        if (ch[k] != ~0u)
+          units[n_units + __popc(there & ((1u << lane) - 1u))] = make_uint2(ch[k] * tv.block_tokens + (at - tv.by_tokens(at) * tv.block_tokens), at);
+        n_units += __popc(there);
       }
-    }
-    if (__any_sync(~0u, turn[0] != 1.0f || turn[1] != 1.0f)) {
-#pragma unroll
-      for (int d = 0; d < D / 8; ++d) {
-        o[d][0] *= turn[0];
-        o[d][1] *= turn[0];
-        o[d][2] *= turn[1];
-        o[d][3] *= turn[1];
-      }
-    }
-    const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
-    float part[2] = {0.0f, 0.0f};
-    uint32_t p[4];
-#pragma unroll
-    for (int n = 0; n < 2; ++n) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = exp2_(s[0][n][e] - base[e >> 1]);
-        s[0][n][e] = x;
-        part[e >> 1] += x;
-      }
-      p[2 * n] = pack2<T>(s[0][n][0], s[0][n][1]);
-      p[2 * n + 1] = pack2<T>(s[0][n][2], s[0][n][3]);
-    }
-    l[0] += part[0];
-    l[1] += part[1];
-    if (kWeights) {
-      float* const grain = grain_at(a, w, at / 16u);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float sum = quad_sum(part[h]);
-        const uint32_t r = lane / 4 + h * 8;
-        if ((lane & 3) == 0 && r < w.rows) grain[r] = base[h] + log2_(sum);
-      }
-    }
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) {
-      uint32_t b[4];
-      const uint32_t c = 2 * d + (lane >> 4);
-      ldmatrix4t(b, v_at + c / 8 * S::kPanelBytes + (((c & 7) ^ (v_row & 7)) * 16));
-      mma<T>(o[2 * d], p, b[0], b[1]);
-      mma<T>(o[2 * d + 1], p, b[2], b[3]);
     }
     __syncwarp();
-    issue(j + S::kSlots, slot);
-    if (++slot == S::kSlots) {
-      slot = 0;
-      parity ^= 1u;
+    // unit j into a slot, a lane for each box: panels of K, then of V
+    auto issue = [&](uint32_t j, uint32_t to) {
+      if (j >= n_units) return;
+      const uint32_t b = smem_address(bar + to);
+      if (lane == 0) bar_expect(b, S::kUnitBytes);
+      __syncwarp();
+      if (lane < 2 * S::kPanels) tma_box(smem_address(ring + to * S::kUnitBytes + lane * S::kPanelBytes), &map, box_x, (int32_t)units[j].x + box_y, b);
+    };
+#pragma unroll
+    for (int k = 0; k < S::kSlots; ++k) issue(k, slot + k < S::kSlots ? slot + k : slot + k - S::kSlots);
+    // queries straight into the operands' registers: rows lane / 4 and 8 further on, elements 2 (lane % 4) and 8 further on
+    uint32_t q[D / 16][4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t r = lane / 4 + h * 8;
+      const bool there = r < w.rows;
+      uint32_t seq = 0, head = 0;
+      if (there) row_of(a, w, r, seq, head);
+      const uint16_t* const src = static_cast<const uint16_t*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head + (lane & 3) * 2;
+      const bool words = (reinterpret_cast<uintptr_t>(src) & 3u) == 0;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint16_t* const x = src + k * 16 + e * 8;
+          q[k][h + 2 * e] = !there ? 0u : words ? *reinterpret_cast<const uint32_t*>(x) : (uint32_t)x[0] | (uint32_t)x[1] << 16;
+        }
+    }
+
+    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[j][e] = 0.0f;
+    for (uint32_t j = 0; j < n_units; ++j) {
+      ok = __all_sync(~0u, bar_wait(smem_address(bar + slot), parity, gave_up, tv.status));
+      if (!ok) break;
+      uint8_t* const unit = ring + slot * S::kUnitBytes;
+      const uint32_t in_ring = slot * S::kUnitBytes;
+      const uint32_t at = units[j].y, left = w.to - at;
+      const bool tail = left < (uint32_t)kUnit;
+      if (tail) {
+        // what lies behind the last token would meet probabilities of zero: it may be anything
+        for (uint32_t x = lane; x < (kUnit - left) * S::kPanels * 8u; x += 32u) {
+          const uint32_t tok = left + x / (S::kPanels * 8u), c = x % (S::kPanels * 8u);
+          *reinterpret_cast<uint4*>(unit + (S::kPanels + c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+        }
+        __syncwarp();
+      }
+      // scores, the even and the odd steps of the sum on their own
+      float s[2][2][4];
+#pragma unroll
+      for (int x = 0; x < 16; ++x) s[x / 8][x / 4 % 2][x % 4] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        uint32_t b[4];
+        ldmatrix4(b, k_off[k % 4] + in_ring + k / 4 * S::kPanelBytes);
+        mma<T>(s[k & 1][0], q[k], b[0], b[1]);
+        mma<T>(s[k & 1][1], q[k], b[2], b[3]);
+      }
+      float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[0][n][e] = (s[0][n][e] + s[1][n][e]) * a.scale2;
+          if (tail && n * 8u + (lane & 3) * 2u + (e & 1) >= left) s[0][n][e] = -INFINITY;
+          top[e >> 1] = fmaxf(top[e >> 1], s[0][n][e]);
+        }
+      float turn[2] = {1.0f, 1.0f};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float mx = quad_max(top[h]);
+        if (mx > m[h]) {
+          turn[h] = exp2_(m[h] - mx);
+          m[h] = mx;
+          l[h] *= turn[h];
+        }
+      }
+      if (__any_sync(~0u, turn[0] != 1.0f || turn[1] != 1.0f)) {
+#pragma unroll
+        for (int d = 0; d < D / 8; ++d) {
+          o[d][0] *= turn[0];
+          o[d][1] *= turn[0];
+          o[d][2] *= turn[1];
+          o[d][3] *= turn[1];
+        }
+      }
+      const float base[2] = {m[0] == -INFINITY ? 0.0f : m[0], m[1] == -INFINITY ? 0.0f : m[1]};
+      float part[2] = {0.0f, 0.0f};
+      uint32_t p[4];
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = exp2_(s[0][n][e] - base[e >> 1]);
+          s[0][n][e] = x;
+          part[e >> 1] += x;
+        }
+        p[2 * n] = pack2<T>(s[0][n][0], s[0][n][1]);
+        p[2 * n + 1] = pack2<T>(s[0][n][2], s[0][n][3]);
+      }
+      l[0] += part[0];
+      l[1] += part[1];
+      if (kWeights) {
+        float* const grain = grain_at(a, w, at / 16u);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float sum = quad_sum(part[h]);
+          const uint32_t r = lane / 4 + h * 8;
+          if ((lane & 3) == 0 && r < w.rows) grain[r] = base[h] + log2_(sum);
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < D / 16; ++d) {
+        uint32_t b[4];
+        ldmatrix4t(b, v_off[d % 4] + in_ring + d / 4 * S::kPanelBytes);
+        mma<T>(o[2 * d], p, b[0], b[1]);
+        mma<T>(o[2 * d + 1], p, b[2], b[3]);
+      }
+      __syncwarp();
+      issue(j + S::kSlots, slot);
+      if (++slot == S::kSlots) {
+        slot = 0;
+        parity ^= 1u;
+      }
+    }
+    if (!ok) break;
+    const uint32_t part = part_of(a, w);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float sum = quad_sum(l[h]);
+      const uint32_t r = lane / 4 + h * 8;
+      if (r >= w.rows) continue;
+      uint32_t seq, head;
+      row_of(a, w, r, seq, head);
+      const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j) put2<T>(a, seq, head, part, j * 8 + (lane & 3) * 2, o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
+      if ((lane & 3) == 0) put_lse(a, seq, head, part, sum != 0.0f ? m[h] + log2_(sum) : -INFINITY);
     }
   }
   if (!ok) {
     // copies in flight end before the memory is given back
     for (uint32_t k = 0; k < 1u << 16; ++k) asm volatile("nanosleep.u32 1000;");
-  }
-  const uint32_t part = part_of(a, w);
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float sum = quad_sum(l[h]);
-    const uint32_t r = lane / 4 + h * 8;
-    if (r >= w.rows) continue;
-    uint32_t seq, head;
-    row_of(a, w, r, seq, head);
-    const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;
-#pragma unroll
-    for (int j = 0; j < D / 8; ++j) put2<T>(a, seq, head, part, j * 8 + (lane & 3) * 2, o[j][2 * h] * inv, o[j][2 * h + 1] * inv);
-    if ((lane & 3) == 0) put_lse(a, seq, head, part, sum != 0.0f ? m[h] + log2_(sum) : -INFINITY);
   }
 }
 
@@ -263,15 +270,15 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_ti
   const TableView& tv = a.tv;
   CUtensorMap map;
   if (!block_map(tv, D, kUnit, &map)) return cudaErrorInvalidValue;
-  const uint64_t rows = (uint64_t)a.max_members * a.group, tile = 16;
-  const uint64_t np = prefix ? (rows + tile - 1) / tile * a.chunks[0] * tv.heads * a.n_groups : 0;
-  const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
+  const uint64_t np = prefix ? (uint64_t)a.chunks[0] * tv.heads * a.n_groups : 0;
+  const uint64_t ns = suffix ? (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
   if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
   auto* kernel = a.weight ? stream_kernel<T, D, true> : stream_kernel<T, D, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_overlapped_smem(kernel, (unsigned)((np + ns + kStreamWarps - 1) / kStreamWarps), (unsigned)kStreamWarps * 32, S::kSmem, s, a, map,
+  const uint64_t ctas = (np + ns + kStreamWarps - 1) / kStreamWarps, most = (uint64_t)sm_count() * S::kCtas;
+  return launch_overlapped_smem(kernel, (unsigned)(ctas < most ? ctas : most), (unsigned)kStreamWarps * 32, S::kSmem, s, a, map,
                                 (uint32_t)np, (uint32_t)(np + ns), behind_tiles ? 1u : 0u);
 }
 
@@ -284,7 +291,7 @@ bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, CUtensorMap*
   const cuuint64_t dims[2] = {dk, tv.n * tv.n_chunks * tv.block_tokens}, strides[1] = {(cuuint64_t)dk * 2};
   const cuuint32_t box[2] = {64, box_rows}, steps[2] = {1, 1};
   return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, tv.slab, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows) {

@@ -6,7 +6,7 @@
 // of tokens lies in shared memory as the matrix instructions want it whatever blocks it is made of; a block
 // that is not there is a box outside the tensor, which reads as zeros.
 //
-// Roles: warp 0 looks blocks up and issues the copies, a warp for each row tile issues its matrix
+// Roles: warps 0 and 3 look blocks up and issue the copies, a warp for each row tile issues its matrix
 // instructions, and each further group of four warps is a row tile's softmax, a thread per row: it reads its row
 // of S, keeps maximum and sum, and writes the probabilities over S, from where P V takes them as the operand
 // in tensor memory.  With two row tiles (kTiles == 2) the tensor cores work on one's products while the
@@ -126,7 +126,7 @@ struct Shape {
   static constexpr int kKBytes = kAPanels * kPanelBytes, kVBytes = kBPanels * kPanelBytes;
   static constexpr int kQBytes = kTiles * kQPanels * 128 * 128;
   static constexpr int kMasks = 8;                          // see the softmax
-  static constexpr int kFirst = kTiles == 2 ? 4 : 2;        // first warp of the softmax
+  static constexpr int kFirst = 4;                          // first warp of the softmax
   static constexpr int kThreads = (kFirst + 4 * kTiles) * 32;
   // tensor memory columns: outputs, then scores, then Q
   static constexpr int kSlots = 2 * kTiles;                 // of scores: two for each row tile, in turn
@@ -342,16 +342,21 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   volatile uint32_t* const gave_up = &ctl->gave_up;
   uint32_t* const status = tv.status;
 
-  if (warp == 0) {
-    // ---- blocks ----
+  if (warp == 0 || warp == 3) {
+    // ---- blocks: a warp for each part of the stages ----
     if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    const int part = warp == 0 ? 0 : 1;
+    const uint32_t bytes = part ? S::kVBytes : S::kKBytes, panels = part ? S::kBPanels : S::kAPanels;
+    const int32_t values = part && !S::kLatent ? (int32_t)(tv.heads * tv.block_tokens) : 0;
     // boxes of a tile; the lanes look the blocks of 32 of them up at a time, before they are needed
     const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box, ahead = 32u / boxes;
-    auto look = [&](uint32_t t) {   // of tiles t .. t + ahead - 1: the chunk of box lane % boxes of tile t + lane / boxes
-      const uint32_t box = t * boxes + lane, at = w.from + box * rows_per_box;
-      return (uint32_t)lane < boxes * ahead && at < w.to ? tv.chunk((uint64_t)w.seg.row + tv.by_tokens(at), w.head) : ~0u;
+    auto look = [&](uint32_t t) {   // of tiles t .. t + ahead - 1: the place of box lane % boxes of tile t + lane / boxes
+      const uint32_t at = w.from + (t * boxes + lane) * rows_per_box;
+      if ((uint32_t)lane >= boxes * ahead || at >= w.to) return outside;
+      const uint32_t b = tv.by_tokens(at), ch = tv.chunk((uint64_t)w.seg.row + b, w.head);
+      return ch == ~0u ? outside : ch * tv.block_tokens + at - b * tv.block_tokens;
     };
-    uint32_t next = look(0), now = ~0u;
+    uint32_t next = look(0), now = outside;
     bool ok = true;
     for (uint32_t t = 0; t < n_tiles && ok; ++t) {
       const uint32_t st = t % S::kStages, round = t / S::kStages;
@@ -359,38 +364,33 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         now = next;
         if (t + ahead < n_tiles) next = look(t + ahead);
       }
-      const uint32_t first = t % ahead * boxes;
-      const uint32_t ch = __shfl_sync(~0u, now, first + lane % boxes);
-      const uint32_t tile0 = w.from + t * S::kTok;
+      const uint32_t first = t % ahead * boxes, tile0 = w.from + t * S::kTok;
       uint32_t bits[S::kTok / 32];
+      if (part == 0) {
 #pragma unroll
-      for (int m = 0; m < S::kTok / 32; ++m) {
-        const uint32_t tok = m * 32 + lane;
-        bits[m] = __ballot_sync(~0u, __shfl_sync(~0u, ch, tok / rows_per_box) != ~0u && tile0 + tok < w.to);
-      }
-      const uint32_t at = tile0 + lane * rows_per_box;
-      const uint32_t in_block = at - tv.by_tokens(at) * tv.block_tokens;
-      const int32_t y = (int32_t)(ch != ~0u ? ch * tv.block_tokens + in_block : outside);
-      uint8_t* const k_dst = ring + st * (S::kKBytes + S::kVBytes);
-#pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        if (round) ok = bar_wait(smem_address(part ? &ctl->v_empty[st] : &ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
-        ok = __all_sync(~0u, ok);
-        if (!ok) break;
-        const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
-        if (lane == 0) {
-          if (part == 0) {   // (ahead of the copies that the scores wait for)
-#pragma unroll
-            for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
-          }
-          bar_expect(bar, part ? S::kVBytes : S::kKBytes);
+        for (int m = 0; m < S::kTok / 32; ++m) {
+          const uint32_t tok = m * 32 + lane;
+          bits[m] = __ballot_sync(~0u, __shfl_sync(~0u, now, first + tok / rows_per_box) != outside && tile0 + tok < w.to);
         }
-        __syncwarp();
-        const int32_t yp = part && !S::kLatent && ch != ~0u ? y + (int32_t)(tv.heads * tv.block_tokens) : y;
-        const uint32_t dst = smem_address(k_dst) + (part ? S::kKBytes : 0) + lane * rows_per_box * 128u;
-        if ((uint32_t)lane < boxes)
-          for (int p = 0; p < (part ? S::kBPanels : S::kAPanels); ++p)
-            tma_box(dst + p * S::kPanelBytes, &map, panel_at<S>(part, p, col0), yp, bar);
+      }
+      if (round) ok = bar_wait(smem_address(part ? &ctl->v_empty[st] : &ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
+      ok = __all_sync(~0u, ok);
+      if (!ok) break;
+      const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
+      if (lane == 0) {
+        if (part == 0) {   // (ahead of the copies that the scores wait for)
+#pragma unroll
+          for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
+        }
+        bar_expect(bar, bytes);
+      }
+      __syncwarp();
+      const uint32_t dst = smem_address(ring) + st * (S::kKBytes + S::kVBytes) + (part ? S::kKBytes : 0);
+      for (uint32_t x0 = 0; x0 < boxes * panels; x0 += 32u) {      // a lane for each box of each panel
+        const uint32_t x = x0 + lane, p = x / boxes, box = x - p * boxes;
+        const uint32_t at = __shfl_sync(~0u, now, first + box);
+        if (x < boxes * panels)
+          tma_box(dst + p * S::kPanelBytes + box * rows_per_box * 128u, &map, panel_at<S>(part, p, col0), (int32_t)at + (at != outside ? values : 0), bar);
       }
     }
   } else if (warp < S::kFirst) {

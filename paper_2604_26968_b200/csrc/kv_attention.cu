@@ -68,11 +68,14 @@ __global__ void __launch_bounds__(kScoreThreads) fold_weights_kernel(float* scor
 
 // Scores of entries that are FREE, or young, are +inf.
 __global__ void __launch_bounds__(kScoreThreads) keep_young_kernel(EntryState st, uint32_t epoch, int32_t protect) {
-  wait_for_kernel_ahead();
   const uint64_t i = ((uint64_t)blockIdx.x * kScoreThreads + threadIdx.x) * 4u;
+  bool keep[4] = {false, false, false, false};
   if (i + 4u <= st.n) {
     const uchar4 s = *reinterpret_cast<const uchar4*>(st.state + i);
-    bool keep[4] = {s.x != KV_STATE_RESIDENT, s.y != KV_STATE_RESIDENT, s.z != KV_STATE_RESIDENT, s.w != KV_STATE_RESIDENT};
+    keep[0] = s.x != KV_STATE_RESIDENT;
+    keep[1] = s.y != KV_STATE_RESIDENT;
+    keep[2] = s.z != KV_STATE_RESIDENT;
+    keep[3] = s.w != KV_STATE_RESIDENT;
     if (protect > 0) {
       const uint4 l = *reinterpret_cast<const uint4*>(st.last_epoch + i);
       keep[0] = keep[0] || (int32_t)(epoch - l.x) < protect;
@@ -80,13 +83,14 @@ __global__ void __launch_bounds__(kScoreThreads) keep_young_kernel(EntryState st
       keep[2] = keep[2] || (int32_t)(epoch - l.z) < protect;
       keep[3] = keep[3] || (int32_t)(epoch - l.w) < protect;
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (keep[k]) st.score[i + k] = INFINITY;
-    return;
+  } else {
+    for (uint64_t j = i; j < st.n; ++j)
+      keep[j - i] = st.state[j] != KV_STATE_RESIDENT || (protect > 0 && (int32_t)(epoch - st.last_epoch[j]) < protect);
   }
-  for (uint64_t j = i; j < st.n; ++j)
-    if (st.state[j] != KV_STATE_RESIDENT || (protect > 0 && (int32_t)(epoch - st.last_epoch[j]) < protect)) st.score[j] = INFINITY;
+  wait_for_kernel_ahead();      // (what is read above was there before the kernel ahead began; it writes scores)
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (keep[k]) st.score[i + k] = INFINITY;
 }
 
 }  // namespace

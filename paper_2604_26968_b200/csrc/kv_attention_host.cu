@@ -51,7 +51,7 @@ constexpr uint32_t kTileRows = 17;
 struct Split {
   bool tiles[2], stream[2];
   uint32_t chunk_tokens[2], chunks[2], per_chunk[2], n_parts, grain_tokens, grains[2];
-  uint64_t lse_at, grain_at[2], bytes;
+  uint64_t lse_at, total_at, grain_at[2], bytes;
 };
 
 // Chunks of a segment of `most` tokens when `ctas` row tiles are split alike and `slots` CTAs run at a time: the
@@ -107,8 +107,13 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
       out->per_chunk[k] = !mla && rows <= 128 ? 2 : 1;
       split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
     } else if (out->stream[k]) {
-      split_segment(segs, most, kStreamUnit, kSms * stream_warps(dk), 3, kStreamTokens, !shared, &out->chunk_tokens[k],
-                    &out->chunks[k]);
+      // a warp's chunk: enough of them for all warps if runs are as long as these bounds for six parts in ten, 8 to 32 units
+      const uint64_t units = ((uint64_t)most + kStreamUnit - 1) / kStreamUnit;
+      uint64_t per = segs * units * 12 / 10 / (kSms * stream_warps(dk));
+      per = per < 8 ? 8 : per > 32 ? 32 : per;
+      per = (units + (units + per - 1) / per - 1) / ((units + per - 1) / per);    // the same number of chunks, evenly
+      out->chunk_tokens[k] = (uint32_t)(per * kStreamUnit);
+      out->chunks[k] = (uint32_t)((units + per - 1) / per);
     } else {
       const uint64_t tile = mla ? 64 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
       split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
@@ -121,6 +126,7 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
   auto take = [&at](unsigned __int128 bytes) { const uint64_t o = (uint64_t)at; at = (at + bytes + 255) / 256 * 256; return o; };
   if (out->n_parts > 1) take(rows * out->n_parts * dv * 4);
   out->lse_at = take(rows * out->n_parts * 4);
+  out->total_at = take(weights ? rows * 4 : 0);
   for (int k = 0; k < 2; ++k) {
     const uint32_t most = k == 0 ? (shared ? max_prefix : 0) : max_suffix;
     out->grains[k] = (uint32_t)(((uint64_t)most + out->grain_tokens - 1) / out->grain_tokens);
@@ -209,6 +215,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   a.direct = sp.n_parts == 1;
   a.part_o = reinterpret_cast<float*>(scratch);
   a.part_lse = reinterpret_cast<float*>(scratch + sp.lse_at);
+  a.total = reinterpret_cast<float*>(scratch + sp.total_at);
   a.grain_tokens = sp.grain_tokens;
   a.weight = reinterpret_cast<unsigned long long*>(d->d_weight);
   return pool_cuda_error(p, launch_attend(a, d->dtype, v.variant[q] == KV_MLA, S(stream)));

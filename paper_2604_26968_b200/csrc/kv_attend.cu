@@ -468,6 +468,7 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
 // ---- parts to outputs, grains to weights -------------------------------------------------------------
 
 constexpr int kFinishThreads = 256, kFinishRows = kFinishThreads / 32;
+constexpr uint32_t kWeightRows = 256;
 
 // The parts of a sequence: np of its group's prefix, ns of its suffix, the latter behind the places of all prefix chunks.
 struct Parts {
@@ -566,8 +567,8 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
   join_rows<T>(a, (uint64_t)blockIdx.x * kFinishRows + threadIdx.x / 32);
 }
 
-// Weight of the blocks of prefixes (the first prefix_blocks items) and suffixes: the sum over a block's rows of what the kernels have
-// left for its grains, taken from the rows' sums; `lanes` threads a block.
+// Weight of the blocks of prefixes (the first prefix_ctas CTAs) and suffixes: the sum over a block's rows of what the kernels have
+// left for its grains, taken from the rows' sums; `lanes` threads for a block and kWeightRows of its rows.
 __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_constant__ AttendArgs a, uint32_t prefix_ctas, uint32_t prefix_lanes,
                                                                uint32_t suffix_lanes) {
   const int kind = blockIdx.x < prefix_ctas ? kKindPrefix : kKindSuffix;
@@ -575,8 +576,9 @@ __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_con
   const uint64_t item = ((uint64_t)(blockIdx.x - (kind == kKindPrefix ? 0u : prefix_ctas)) * kFinishThreads + threadIdx.x) / lanes;
   const uint32_t lane = threadIdx.x % lanes;
   const uint32_t most_blocks = ((kind == kKindPrefix ? a.max_prefix : a.max_suffix) + a.tv.block_tokens - 1u) / a.tv.block_tokens;
-  const uint64_t sh = item / most_blocks;
-  const uint32_t b = (uint32_t)(item - sh * most_blocks);
+  const uint32_t most_rows = kind == kKindPrefix ? a.max_members * a.group : a.group, shares = (most_rows + kWeightRows - 1u) / kWeightRows;
+  const uint64_t sb = item / shares, sh = sb / most_blocks;
+  const uint32_t row0 = (uint32_t)(item - sb * shares) * kWeightRows, b = (uint32_t)(sb - sh * most_blocks);
   const uint64_t index = sh / a.tv.heads;
   const uint32_t head = (uint32_t)(sh - index * a.tv.heads);
   unsigned long long w = 0;
@@ -596,7 +598,8 @@ __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_con
     }
     const uint32_t from = b * a.tv.block_tokens;
     const uint64_t at = (uint64_t)seg.row + b;
-    const bool there = from < seg.tokens && rows && a.tv.chunk(at, head) != ~0u;
+    rows = min(rows, row0 + kWeightRows);
+    const bool there = from < seg.tokens && row0 < rows && a.tv.chunk(at, head) != ~0u;
     if (there) handle = a.tv.table[(at * a.tv.layers + a.tv.layer) * a.tv.heads + head];
     wait_for_kernel_ahead();      // (what is read above was there before the call's first kernel began)
     if (there) {
@@ -606,7 +609,7 @@ __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_con
       const float* const grain = a.grain[kind] + (index * a.tv.heads + head) * (uint64_t)a.grains[kind] * stride;
       float sum = 0.0f;
 #pragma unroll 4
-      for (uint32_t r = lane; r < rows; r += lanes) {
+      for (uint32_t r = row0 + lane; r < rows; r += lanes) {
         const uint32_t member = r / a.group;
         const float lse = total[(uint64_t)(seq0 + member) * a.q_heads + head * a.group + (r - member * a.group)];
         if (lse == -INFINITY) continue;
@@ -698,7 +701,7 @@ cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t 
     const uint64_t blocks = ((uint64_t)most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
     const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
     while (lanes[kind] < 32u && lanes[kind] < r) lanes[kind] *= 2u;
-    ctas[kind] = ((uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks * lanes[kind] + kFinishThreads - 1) / kFinishThreads;
+    ctas[kind] = ((uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks * ((r + kWeightRows - 1u) / kWeightRows) * lanes[kind] + kFinishThreads - 1) / kFinishThreads;
   }
   if (ctas[0] + ctas[1] == 0) return cudaSuccess;
   if (ctas[0] + ctas[1] > 0x7fffffffull) return cudaErrorInvalidValue;

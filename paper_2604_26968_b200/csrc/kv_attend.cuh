@@ -132,7 +132,7 @@ cudaError_t launch_attend(const AttendArgs& a, int dtype, bool mla, cudaStream_t
 bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows, bool weights);
 cudaError_t launch_attend_tiles(const AttendArgs& a, int dtype, bool mla, bool prefix, bool suffix, cudaStream_t s);
 
-// kv_attend_stream.cu: the same for up to 16 rows.  behind_tiles: launch_attend_tiles went ahead in this call, and the two
+// kv_attend_stream.cu: the same for up to 32 rows (two row tiles of 16, each a stream of its own).  behind_tiles: launch_attend_tiles went ahead in this call, and the two
 // may run side by side.
 bool stream_takes(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows);
 uint32_t stream_warps(uint32_t dk);   // of an SM

@@ -58,16 +58,15 @@ struct Item {
 // False: there is nothing to do.
 template <bool by_chunk = false>
 __device__ __forceinline__ bool item_of(const AttendArgs& a, int kind, uint32_t i, uint32_t row_tile, Item& w, bool tell) {
-  uint32_t rt = 0;
-  if (by_chunk) {      // (one row tile)
+  const uint32_t most = kind == kKindPrefix ? a.max_members * a.group : a.group;
+  const uint32_t tiles = (most + row_tile - 1u) / row_tile;
+  const uint32_t rt = i % tiles;
+  i /= tiles;
+  if (by_chunk) {
     const uint32_t segments = (kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads;
     w.chunk = i / segments;
     i -= w.chunk * segments;
   } else {
-    const uint32_t most = kind == kKindPrefix ? a.max_members * a.group : a.group;
-    const uint32_t tiles = (most + row_tile - 1u) / row_tile;
-    rt = i % tiles;
-    i /= tiles;
     w.chunk = i % a.chunks[kind];
     i /= a.chunks[kind];
   }

@@ -270,8 +270,8 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_ti
   const TableView& tv = a.tv;
   CUtensorMap map;
   if (!block_map(tv, D, kUnit, &map)) return cudaErrorInvalidValue;
-  const uint64_t np = prefix ? (uint64_t)a.chunks[0] * tv.heads * a.n_groups : 0;
-  const uint64_t ns = suffix ? (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
+  const uint64_t np = prefix ? ((uint64_t)a.max_members * a.group + 15) / 16 * a.chunks[0] * tv.heads * a.n_groups : 0;
+  const uint64_t ns = suffix ? (a.group + 15) / 16 * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
   if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
   auto* kernel = a.weight ? stream_kernel<T, D, true> : stream_kernel<T, D, false>;

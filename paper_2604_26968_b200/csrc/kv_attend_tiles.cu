@@ -244,7 +244,8 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w,
   };
   auto turned = [&](uint4 v) { return make_uint4((v.x & q_bits) ^ q_sign, (v.y & q_bits) ^ q_sign, (v.z & q_bits) ^ q_sign, (v.w & q_bits) ^ q_sign); };
   constexpr int kVecs = S::kQPanels * 8;    // 16-byte vectors of a row
-  constexpr int kBatch = 8;
+  constexpr int kBatch = kVecs % 20 == 0 ? 20 : kVecs < 16 ? kVecs : 16;   // on their way at a time
+  static_assert(kVecs % kBatch == 0, "vectors of a row");
 #pragma unroll 1
   for (int k0 = 0; k0 < kVecs; k0 += kBatch) {
     uint4 v[kBatch];
@@ -264,19 +265,23 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w,
     const uint32_t row = lane_at + (thread & 31u);
     const T* const src = source(row < w.rows ? row : 0u);
 #pragma unroll 1
-    for (int c = 0; c < S::kQTmem / 64; ++c) {
-      uint32_t v[32];
+    for (int c = 0; c < S::kQTmem / 64; c += 2) {
+      uint4 x[16];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (row < w.rows) x = load8(src + c * 64 + e * 8);
-        x = turned(x);
-        v[4 * e] = x.x;
-        v[4 * e + 1] = x.y;
-        v[4 * e + 2] = x.z;
-        v[4 * e + 3] = x.w;
+      for (int e = 0; e < 16; ++e) x[e] = row < w.rows ? load8(src + c * 64 + e * 8) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t v[32];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint4 y = turned(x[half * 8 + e]);
+          v[4 * e] = y.x;
+          v[4 * e + 1] = y.y;
+          v[4 * e + 2] = y.z;
+          v[4 * e + 3] = y.w;
+        }
+        tmem_store(tmem + (lane_at << 16) + S::kQAt + (c + half) * 32, v);
       }
-      tmem_store(tmem + (lane_at << 16) + S::kQAt + c * 32, v);
     }
     tmem_wait_store();
   }

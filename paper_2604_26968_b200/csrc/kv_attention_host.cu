@@ -47,32 +47,50 @@ TableView table_view(const PoolView& v, int32_t q, int32_t layer, const uint32_t
 // How a call's work is split: tokens of a chunk and chunks, for prefixes and suffixes.
 constexpr uint32_t kSms = 148;
 // Rows from which on a segment goes to the tensor cores' 128-row tiles.
-constexpr uint32_t kTileRows = 17;
+constexpr uint32_t kTileRows = 33;
 struct Split {
   bool tiles[2], stream[2];
   uint32_t chunk_tokens[2], chunks[2], per_chunk[2], n_parts, grain_tokens, grains[2];
   uint64_t lse_at, total_at, grain_at[2], bytes;
 };
 
-// Chunks of a segment of `most` tokens when `ctas` row tiles are split alike and `slots` CTAs run at a time: the
-// split whose turns, times the tiles of a chunk and what a CTA costs beside them (`extra` tiles), are fewest.  alone: no
-// other segments' parts are joined with these, so that one part needs no second launch (as long as `extra` twice).
-void split_segment(uint64_t ctas, uint32_t most, uint32_t tile, uint32_t slots, uint32_t extra, uint64_t limit, bool alone,
-                   uint32_t* chunk, uint32_t* chunks) {
-  if (!ctas) ctas = 1;
-  const uint64_t tiles = ((uint64_t)most + tile - 1) / tile, most_tiles = limit / tile;
-  uint64_t n = (tiles + most_tiles - 1) / most_tiles, best = ~0ull, best_tiles = 1;
-  const uint64_t last = n + 2 * slots / ctas + 1;
-  for (; n <= last && n <= tiles; ++n) {
-    const uint64_t per = (tiles + n - 1) / n, parts = (tiles + per - 1) / per;
-    const uint64_t cost = (ctas * parts + slots - 1) / slots * (per + extra) + (alone && parts > 1 ? 2 * extra : 0);
-    if (cost < best) {
-      best = cost;
-      best_tiles = per;
+// How segments of `tiles` tiles (at most) are cut when `ctas` row tiles are split alike: `per` tiles a chunk.
+struct Cut {
+  uint64_t ctas, tiles, most_per, per;
+  uint64_t chunks() const { return ctas ? (tiles + per - 1) / per : 0; }
+};
+// The cuts of prefixes and suffixes that one launch runs through, `slots` CTAs at a time, prefixes first: those for which the
+// longer of the longest CTA and an even share of all of them is shortest.  A CTA costs `extra` tiles beside its own; suffixes
+// are taken to be as long as their bound for six parts in ten; a part more than one in all costs another launch.
+void cut(Cut& p, Cut& s, uint64_t slots, uint64_t extra, bool alone) {
+  uint64_t best = ~0ull, best_p = 1, best_s = 1;
+  auto first = [](const Cut& c) { return c.ctas ? (c.tiles + c.most_per - 1) / c.most_per : 1; };
+  auto last = [slots](const Cut& c) { return c.ctas ? 2 * slots / c.ctas + 1 : 0; };
+  for (uint64_t np = first(p); np <= first(p) + last(p); ++np) {
+    p.per = p.ctas ? (p.tiles + np - 1) / np : 1;
+    for (uint64_t ns = first(s); ns <= first(s) + last(s); ++ns) {
+      s.per = s.ctas ? (s.tiles + ns - 1) / ns : 1;
+      const uint64_t n_p = p.ctas * p.chunks(), n_s = s.ctas * s.chunks(), longest = (n_p && p.per > s.per) || !n_s ? p.per : s.per;
+      uint64_t cost;
+      if (!n_p || !n_s) {
+        cost = (n_p + n_s + slots - 1) / slots * (longest + extra);
+      } else {
+        const uint64_t all = n_p * (p.per + extra) + s.ctas * (s.tiles * 6 / 10) + n_s * extra;
+        cost = all / slots + (n_p + n_s > slots ? ((p.per < s.per ? p.per : s.per) + extra) / 2 : 0);
+        if (cost < longest + extra) cost = longest + extra;
+      }
+      if (alone && n_p + n_s > p.ctas + s.ctas) cost += 2 * extra;
+      if (cost < best) {
+        best = cost;
+        best_p = p.per;
+        best_s = s.per;
+      }
+      if (s.per == 1) break;
     }
+    if (p.per == 1) break;
   }
-  *chunk = (uint32_t)(best_tiles * tile);
-  *chunks = (uint32_t)((tiles + best_tiles - 1) / best_tiles);
+  p.per = best_p;
+  s.per = best_s;
 }
 
 bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_seqs, uint32_t n_groups, uint32_t max_suffix,
@@ -93,30 +111,43 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
   const uint64_t slab_rows = v.geom[q].n * v.geom[q].n_chunks * bt;
   const bool streams = stream_takes(dk, dv, mla, bt, slab_rows);
   const bool fits = tiles_take(dk, dv, mla, bt, slab_rows, weights);
+  uint64_t limit = (uint64_t)kMaxChunkBlocks * bt / 64 * 64;   // most tokens of a chunk
+  if (limit < 64) limit = 64;
+  if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
+  // prefix and suffix, by the kernels that take them: tiles, streams, the rest
+  Cut tiles[2] = {}, rest[2] = {};
+  uint64_t rest_slots = 2 * kSms;
   for (int k = 0; k < 2; ++k) {
     if (k == 0 && !shared) continue;
     const uint64_t rows = k == 0 ? prefix_rows : group, segs = (uint64_t)(k == 0 ? n_groups : n_seqs) * heads;
     const uint32_t most = k == 0 ? max_prefix : max_suffix ? max_suffix : 1;
     out->tiles[k] = fits && rows >= kTileRows;
-    uint64_t limit = (uint64_t)kMaxChunkBlocks * bt / 64 * 64;   // most tokens of a chunk
-    if (limit < 64) limit = 64;
-    if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;
-    out->stream[k] = !out->tiles[k] && streams && rows <= 16;
+    out->stream[k] = !out->tiles[k] && streams && rows <= 32;
     if (out->tiles[k]) {
       const uint64_t tile = mla ? 128 : 256;
       out->per_chunk[k] = !mla && rows <= 128 ? 2 : 1;
-      split_segment((rows + tile - 1) / tile * segs * (mla ? 2 : 1), most, 64, kSms, 8, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
+      tiles[k] = Cut{(rows + tile - 1) / tile * segs * (mla ? 2 : 1), ((uint64_t)most + 63) / 64, limit / 64, 1};
     } else if (out->stream[k]) {
       // a warp's chunk: enough of them for all warps if runs are as long as these bounds for six parts in ten, 8 to 32 units
       const uint64_t units = ((uint64_t)most + kStreamUnit - 1) / kStreamUnit;
-      uint64_t per = segs * units * 12 / 10 / (kSms * stream_warps(dk));
+      uint64_t per = (rows + 15) / 16 * segs * units * 12 / 10 / (kSms * stream_warps(dk));
       per = per < 8 ? 8 : per > 32 ? 32 : per;
       per = (units + (units + per - 1) / per - 1) / ((units + per - 1) / per);    // the same number of chunks, evenly
       out->chunk_tokens[k] = (uint32_t)(per * kStreamUnit);
       out->chunks[k] = (uint32_t)((units + per - 1) / per);
     } else {
       const uint64_t tile = mla ? 64 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-      split_segment((rows + tile - 1) / tile * segs, most, 64, mla ? kSms : 2 * kSms, 4, limit, !shared, &out->chunk_tokens[k], &out->chunks[k]);
+      rest[k] = Cut{(rows + tile - 1) / tile * segs, ((uint64_t)most + 63) / 64, limit / 64, 1};
+      if (mla) rest_slots = kSms;
+    }
+  }
+  for (Cut* c : {tiles, rest}) {
+    if (!c[0].ctas && !c[1].ctas) continue;
+    cut(c[0], c[1], c == tiles ? kSms : rest_slots, c == tiles ? 8 : 4, !shared);
+    for (int k = 0; k < 2; ++k) {
+      if (!c[k].ctas) continue;
+      out->chunk_tokens[k] = (uint32_t)(c[k].per * 64);
+      out->chunks[k] = (uint32_t)c[k].chunks();
     }
   }
   out->n_parts = out->chunks[0] * out->per_chunk[0] + out->chunks[1] * out->per_chunk[1];

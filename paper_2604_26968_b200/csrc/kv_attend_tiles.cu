@@ -135,7 +135,9 @@ struct Shape {
   static_assert(kQAt + kQTmem / 2 <= kTmem, "tensor memory");
   static_assert(kTok == 64, "four grains of weight");
   static constexpr int kControl = 1024;
-  static constexpr size_t kSmem = (size_t)kQBytes + kStages * (kKBytes + kVBytes) + kControl + 1024;
+  static constexpr int kOutBytes = kTiles == 2 ? 32768 : 0;    // 4 KB a warp, where its results change places (MLA: in the queries' place)
+  static constexpr size_t kSmem = (size_t)kQBytes + kStages * (kKBytes + kVBytes) + kOutBytes + kControl + 1024;
+  static_assert(kSmem <= 232448, "shared memory of a CTA");
 };
 
 struct Control {   // in shared memory
@@ -232,59 +234,55 @@ __device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_a
   }
 }
 
-// Rows of a row tile's queries into shared memory, as the copies would lay them, and (MLA) their first elements
-// into tensor memory, by the tile's 128 threads.
+// A row tile's queries, a thread for each row: the first elements (MLA) into tensor memory, the others into shared memory as
+// the copies would lay them.  (Short loops: this runs once, and its instructions come from memory.  Written out for all
+// of a row's vectors it took 15,000 cycles.)
 template <typename T, typename S>
-__device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w, uint8_t* q_s, uint32_t tmem, int r, uint32_t thread, uint32_t lane_at,
+__device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w, uint8_t* q_s, uint32_t tmem, int r, uint32_t in_tile, uint32_t lane_at,
                                              uint32_t q_sign, uint32_t q_bits) {
-  auto source = [&](uint32_t row) {
-    uint32_t seq, head;
-    row_of(a, w, row, seq, head);
-    return static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head;
-  };
-  auto turned = [&](uint4 v) { return make_uint4((v.x & q_bits) ^ q_sign, (v.y & q_bits) ^ q_sign, (v.z & q_bits) ^ q_sign, (v.w & q_bits) ^ q_sign); };
-  constexpr int kVecs = S::kQPanels * 8;    // 16-byte vectors of a row
-  constexpr int kBatch = kVecs % 20 == 0 ? 20 : kVecs < 16 ? kVecs : 16;   // on their way at a time
-  static_assert(kVecs % kBatch == 0, "vectors of a row");
+  const uint32_t row = r * 128u + in_tile;
+  const bool there = row < w.rows;
+  uint32_t seq = 0, head = 0;
+  if (there) row_of(a, w, row, seq, head);
+  const T* const src = static_cast<const T*>(a.q) + (int64_t)seq * a.q_seq + (int64_t)head * a.q_head;
+  const bool wide = (reinterpret_cast<uintptr_t>(a.q) & 15u) == 0 && a.q_seq % 8 == 0 && a.q_head % 8 == 0;
+  constexpr int kVecs = S::kDk / 8, kInTmem = S::kQTmem / 8;    // 16-byte vectors of a row
 #pragma unroll 1
-  for (int k0 = 0; k0 < kVecs; k0 += kBatch) {
-    uint4 v[kBatch];
+  for (int c0 = 0; c0 < kVecs; c0 += 8) {                       // a panel at a time
+    uint4 v[8];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const uint32_t x = thread + (k0 + k) * 128u, row = x / kVecs, c = x % kVecs;
-      v[k] = make_uint4(0, 0, 0, 0);
-      if (r * 128u + row < w.rows) v[k] = load8(source(r * 128u + row) + S::kQTmem + c * 8u);
-    }
+    for (int e = 0; e < 8; ++e) v[e] = make_uint4(0, 0, 0, 0);
+    if (there && wide) {
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const uint32_t x = thread + (k0 + k) * 128u, row = x / kVecs, c = x % kVecs;
-      *reinterpret_cast<uint4*>(q_s + (r * S::kQPanels + c / 8u) * 16384u + row * 128u + (((c % 8u) ^ (row & 7u)) * 16u)) = turned(v[k]);
-    }
-  }
-  if (S::kQTmem) {
-    const uint32_t row = lane_at + (thread & 31u);
-    const T* const src = source(row < w.rows ? row : 0u);
+      for (int e = 0; e < 8; ++e) v[e] = reinterpret_cast<const uint4*>(src)[c0 + e];
+    } else if (there) {
 #pragma unroll 1
-    for (int c = 0; c < S::kQTmem / 64; c += 2) {
-      uint4 x[16];
+      for (int e = 0; e < 64; ++e) {
+        const uint32_t x = (uint32_t)reinterpret_cast<const uint16_t*>(src)[c0 * 8 + e] << (e % 2 * 16);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] = row < w.rows ? load8(src + c * 64 + e * 8) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint32_t v[32];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint4 y = turned(x[half * 8 + e]);
-          v[4 * e] = y.x;
-          v[4 * e + 1] = y.y;
-          v[4 * e + 2] = y.z;
-          v[4 * e + 3] = y.w;
-        }
-        tmem_store(tmem + (lane_at << 16) + S::kQAt + (c + half) * 32, v);
+        for (int k = 0; k < 32; ++k)
+          if (k == e / 2) (&v[k / 4].x)[k % 4] |= x;
       }
     }
-    tmem_wait_store();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = make_uint4((v[e].x & q_bits) ^ q_sign, (v[e].y & q_bits) ^ q_sign, (v[e].z & q_bits) ^ q_sign, (v[e].w & q_bits) ^ q_sign);
+    if (c0 < kInTmem) {
+      uint32_t x[32];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        x[4 * e] = v[e].x;
+        x[4 * e + 1] = v[e].y;
+        x[4 * e + 2] = v[e].z;
+        x[4 * e + 3] = v[e].w;
+      }
+      tmem_store(tmem + (lane_at << 16) + S::kQAt + c0 * 4, x);
+    } else {
+      uint8_t* const to = q_s + (r * S::kQPanels + (c0 - kInTmem) / 8) * 16384u + in_tile * 128u;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) *reinterpret_cast<uint4*>(to + ((e ^ (in_tile & 7u)) * 16u)) = v[e];
+    }
   }
+  if (S::kQTmem) tmem_wait_store();
   proxy_fence();
   fence_before();
 }
@@ -298,7 +296,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   uint8_t* const smem = raw + ((1024u - (smem_address(raw) & 1023u)) & 1023u);
   uint8_t* const q_s = smem;
   uint8_t* const ring = smem + S::kQBytes;
-  Control* const ctl = reinterpret_cast<Control*>(ring + S::kStages * (S::kKBytes + S::kVBytes));
+  uint8_t* const outs = S::kOutBytes ? ring + S::kStages * (S::kKBytes + S::kVBytes) : q_s;
+  Control* const ctl = reinterpret_cast<Control*>(ring + S::kStages * (S::kKBytes + S::kVBytes) + S::kOutBytes);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   wait_for_kernel_ahead();
 
@@ -424,7 +423,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       const bool mine = row < w.rows;
       const uint32_t o_at = tmem + (lane_at << 16) + r * S::kCols;
       if (r == 0 || !shared) {
-        load_queries<T, S>(a, w, q_s, tmem, r, threadIdx.x - (S::kFirst + 4 * r) * 32, lane_at, q_sign, q_bits);
+        load_queries<T, S>(a, w, q_s, tmem, r, lane_at + lane, lane_at, q_sign, q_bits);
         bar_arrive(smem_address(&ctl->q_ready[r]));
       }
       float m = -INFINITY, l = 0.0f;
@@ -539,24 +538,44 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         if (mine) row_of(a, w, row, seq, head);
         const uint32_t part = part_of(a, w) + (shared ? r : 0);
         const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+        // A warp's 32 rows x 32 columns at a time change places in shared memory (16-byte chunks of a row exchanged by the row), so
+        // that eight lanes write a row's 128 bytes instead of each a row's 16.
+        uint8_t* const place = outs + (warp - S::kFirst) * 4096;
+        const bool narrow_ok = (reinterpret_cast<uintptr_t>(a.out) & 7u) == 0 && a.out_seq % 4 == 0 && a.out_head % 4 == 0;
+        const uint64_t row_at = !mine ? ~0ull : a.direct ? (uint64_t)((int64_t)seq * a.out_seq + (int64_t)head * a.out_head)
+                                                         : (((uint64_t)seq * a.q_heads + head) * a.n_parts + part) * a.dv;
 #pragma unroll 1
         for (int c = 0; c < S::kCols / 32; ++c) {
           uint32_t o[32];
           tmem_load(o, o_at + c * 32);
           tmem_wait_load();
           tmem_loaded(o);
-          if (!mine) continue;
-          if (a.direct) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 2)
-              put2<T>(a, seq, head, part, col0 + c * 32 + e, __uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv);
-          } else {
-            float* const to = a.part_o + (((uint64_t)seq * a.q_heads + head) * a.n_parts + part) * a.dv + col0 + c * 32;
-#pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4*>(to + e) = make_float4(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv,
-                                                               __uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<float4*>(place + lane * 128 + ((e ^ (lane & 7)) * 16)) =
+                make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv, __uint_as_float(o[4 * e + 2]) * inv,
+                            __uint_as_float(o[4 * e + 3]) * inv);
+          __syncwarp();
+#pragma unroll 2
+          for (int k = 0; k < 8; ++k) {
+            const int of = k * 4 + lane / 8, e = lane % 8;
+            const uint64_t at = (uint64_t)__shfl_sync(~0u, (uint32_t)row_at, of) | (uint64_t)__shfl_sync(~0u, (uint32_t)(row_at >> 32), of) << 32;
+            const float4 v = *reinterpret_cast<const float4*>(place + of * 128 + ((e ^ (of & 7)) * 16));
+            if (at == ~0ull) continue;
+            const uint32_t col = col0 + c * 32 + e * 4;
+            if (!a.direct) {
+              *reinterpret_cast<float4*>(a.part_o + at + col) = v;
+            } else if (narrow_ok) {
+              *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + (int64_t)at + col) = make_uint2(pack2<T>(v.x, v.y), pack2<T>(v.z, v.w));
+            } else {
+              T* const to = static_cast<T*>(a.out) + (int64_t)at + col;
+              to[0] = narrow<T>(v.x);
+              to[1] = narrow<T>(v.y);
+              to[2] = narrow<T>(v.z);
+              to[3] = narrow<T>(v.w);
+            }
           }
+          __syncwarp();
         }
         if (mine && col0 == 0) put_lse(a, seq, head, part, l != 0.0f ? m + log2_(l) : -INFINITY);
       }

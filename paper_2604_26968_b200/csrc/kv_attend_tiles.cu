@@ -192,12 +192,17 @@ __device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_a
   auto wait = [&](unsigned long long* bar, uint32_t parity) {
     return __all_sync(~0u, bar_wait(smem_address(bar), parity, gave_up, status));
   };
+  // both: asked at once, as an answer takes a while even where it is yes
+  auto wait2 = [&](unsigned long long* bar, uint32_t parity, unsigned long long* bar2, uint32_t parity2) {
+    const bool a = bar_test(smem_address(bar), parity), b = bar_test(smem_address(bar2), parity2);
+    if (__all_sync(~0u, a && b)) return true;
+    return wait(bar, parity) && wait(bar2, parity2);
+  };
   auto next_scores = [&](uint32_t i) {
     const uint32_t t = place(i), st = t % S::kStages, parity = (t / S::kStages) & 1;
-    if (!wait(&ctl->k_full[st], parity)) return false;
     // these scores take the place of probabilities that an output of two tiles ago is formed from: products of
     // different accumulators may overlap, so it has to be complete
-    if (i >= 2 && !wait(&ctl->pv_done[r], i & 1)) return false;
+    if (i < 2 ? !wait(&ctl->k_full[st], parity) : !wait2(&ctl->k_full[st], parity, &ctl->pv_done[r], i & 1)) return false;
     fence_after();
     if (elected()) {
       scores(i, t, 0);
@@ -221,8 +226,7 @@ __device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_a
   for (uint32_t i = 0; i < n_tiles; ++i) {
     if (i + 1 < n_tiles && !next_scores(i + 1)) return;
     const uint32_t t = place(i), st = t % S::kStages;
-    if (!S::kLatent && !wait(&ctl->v_full[st], (t / S::kStages) & 1)) return;
-    if (!wait(&ctl->p_ready[2 * r + (i & 1)], (i >> 1) & 1)) return;
+    if (!wait2(&ctl->v_full[st], (t / S::kStages) & 1, &ctl->p_ready[2 * r + (i & 1)], (i >> 1) & 1)) return;
     fence_after();
     if (elected()) {
       output(i, t);
@@ -427,16 +431,15 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         bar_arrive(smem_address(&ctl->q_ready[r]));
       }
       float m = -INFINITY, l = 0.0f;
-      bool ok = true;
       for (uint32_t i = 0; i < my_tiles; ++i) {
         const uint32_t t = shared ? 2u * i + r : i;
         const int slot = 2 * r + (int)(i & 1);
         const uint32_t s_at = tmem + (lane_at << 16) + S::kSAt + slot * S::kTok;
         // (The tile's mask was written ahead of the copies that the scores have waited for.  It is written again eight tiles on,
         // when the scores four tiles on are complete, which have waited for this tile's output.)
-        ok = bar_wait(smem_address(&ctl->s_full[slot]), (i >> 1) & 1, gave_up, status);
-        ok = __all_sync(~0u, ok);
-        if (!ok) break;
+        // A wait that gives up lets the loop run out: every later one returns at once, and nothing leaves its bounds.
+        bar_wait(smem_address(&ctl->s_full[slot]), (i >> 1) & 1, gave_up, status);
+        __syncwarp();
         fence_after();
         uint32_t bits[S::kTok];
         float* const s = reinterpret_cast<float*>(bits);
@@ -456,15 +459,14 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
           for (int e = 0; e < S::kTok; ++e)
             if (!(mask[e / 32] >> (e % 32) & 1u)) s[e] = -INFINITY;
         }
-        float top[4] = {s[0], s[1], s[2], s[3]};
+        float top[8];
 #pragma unroll
-        for (int e = 4; e + 8 <= S::kTok; e += 8) {
+        for (int k = 0; k < 8; ++k) top[k] = fmaxf(s[k], s[k + 8]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) top[k] = max3(top[k], s[e + 2 * k], s[e + 2 * k + 1]);
-        }
+        for (int e = 16; e < S::kTok; e += 16)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], s[S::kTok - 4 + k]);
-        const float mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale2;
+          for (int k = 0; k < 8; ++k) top[k] = max3(top[k], s[e + k], s[e + k + 8]);
+        const float mx = fmaxf(max3(max3(top[0], top[1], top[2]), top[3], top[4]), max3(top[5], top[6], top[7])) * a.scale2;
         // the base follows the maximum when it has grown by 8 (or from nothing)
         float turn_by = 1.0f;
         if (mx > m + 8.0f || (m == -INFINITY && mx > m)) {
@@ -476,9 +478,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         const Pair scale(a.scale2, a.scale2), minus(-base, -base);
         if (i > 0 && __any_sync(~0u, turn_by != 1.0f)) {
           // (no product of this row tile is under way: the next waits for these probabilities)
-          ok = bar_wait(smem_address(&ctl->pv_done[r]), (i - 1) & 1, gave_up, status);
-          ok = __all_sync(~0u, ok);
-          if (!ok) break;
+          bar_wait(smem_address(&ctl->pv_done[r]), (i - 1) & 1, gave_up, status);
+          __syncwarp();
           fence_after();
 #pragma unroll 1
           for (int c = 0; c < S::kCols / 32; ++c) {
@@ -492,12 +493,13 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
           }
           tmem_wait_store();
         }
-#pragma unroll
-        for (int e = 0; e < S::kTok; e += 2) fma2(Pair(s[e], s[e + 1]), scale, minus).get(s[e], s[e + 1]);
         Pair sums[4] = {Pair(0.0f, 0.0f), Pair(0.0f, 0.0f), Pair(0.0f, 0.0f), Pair(0.0f, 0.0f)};
 #pragma unroll
         for (int e = 0; e < S::kTok; e += 2) {
-          const float x = exp2_(s[e]), y = exp2_(s[e + 1]);
+          float x, y;
+          fma2(Pair(s[e], s[e + 1]), scale, minus).get(x, y);
+          x = exp2_(x);
+          y = exp2_(y);
           sums[kWeights ? e / 16 : e / 2 % 4] = add2(sums[kWeights ? e / 16 : e / 2 % 4], Pair(x, y));   // (with weights: by grains)
           bits[e / 2] = pack2<T>(x, y);
         }
@@ -516,9 +518,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         // what lies behind the last token, in its block, would meet probabilities of zero: it may be anything
         const uint32_t left = w.to - (w.from + t * S::kTok);
         if (left < (uint32_t)S::kTok && left % box_rows) {
-          ok = bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
-          ok = __all_sync(~0u, ok);
-          if (!ok) break;
+          bar_wait(smem_address(&ctl->v_full[t % S::kStages]), (t / S::kStages) & 1, gave_up, status);
           uint8_t* const vt = ring + (t % S::kStages) * (S::kKBytes + S::kVBytes) + S::kKBytes;
           const uint32_t end = (left + box_rows - 1u) / box_rows * box_rows;
           for (uint32_t x = lane_at + lane; x < (end - left) * (S::kCols / 8u); x += 128u) {
@@ -530,9 +530,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
         fence_before();
         bar_arrive(smem_address(&ctl->p_ready[slot]));
       }
-      if (ok) ok = bar_wait(smem_address(&ctl->o_done[r]), 0, gave_up, status);
-      ok = __all_sync(~0u, ok);
-      if (ok) {
+      if (__all_sync(~0u, bar_wait(smem_address(&ctl->o_done[r]), 0, gave_up, status))) {
         fence_after();
         uint32_t seq = 0, head = 0;
         if (mine) row_of(a, w, row, seq, head);

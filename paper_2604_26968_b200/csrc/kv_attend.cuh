@@ -129,7 +129,7 @@ constexpr uint32_t kMaxChunkTokens = 4096, kMaxChunkBlocks = 256;   // most a CT
 cudaError_t launch_attend(const AttendArgs& a, int dtype, bool mla, cudaStream_t s);
 
 // kv_attend_tiles.cu: whether it takes a geometry, and its part of launch_attend
-bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows, bool weights);
+bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows);
 cudaError_t launch_attend_tiles(const AttendArgs& a, int dtype, bool mla, bool prefix, bool suffix, cudaStream_t s);
 
 // kv_attend_stream.cu: the same for up to 32 rows (two row tiles of 16, each a stream of its own).  behind_tiles: launch_attend_tiles went ahead in this call, and the two

@@ -2,7 +2,7 @@
 // by which the kernels here and in kv_attend_tiles.cu copy blocks).
 //
 // A warp takes chunks of segments, one after the other, in units of 16 tokens of one block; a block that is not in HBM is no unit.  It has a ring
-// of units of its own, filled by TMA (a box of 16 rows x 64 elements, swizzled, for each panel of K and V) which it issues
+// of units of its own, filled by TMA (one box of 16 rows: K's panels of 64 elements, swizzled, then V's) which it issues
 // itself as it empties them: no warp waits for another.  A unit's scores (16 rows x 16 tokens) and output are mma.sync
 // products whose operands come from the ring by ldmatrix, free of bank conflicts thanks to the swizzle.  The output is
 // rescaled only when a maximum has grown.
@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
     for (int b = 0; b < S::kSlots; ++b) bar_init(smem_address(bar + b), 1);
     *gave_up = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    proxy_fence();
   }
   __syncwarp();
   // lanes' places in the ring's operands: rows of a unit's panels, 16-byte chunks exchanged by the row
@@ -69,7 +69,6 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
     k_off[c] = smem_address(ring) + k_row * 128 + (((2 * c + (lane >> 3 & 1)) ^ (k_row & 7)) * 16);
     v_off[c] = smem_address(ring) + S::kPanels * S::kPanelBytes + v_row * 128 + (((2 * c + (lane >> 4)) ^ (v_row & 7)) * 16);
   }
-  const int32_t box_x = (lane % S::kPanels) * 64, box_y = lane / S::kPanels ? (int32_t)(tv.heads * tv.block_tokens) : 0;
   uint32_t slot = 0, parity = 0;
   bool ok = true;
   for (uint32_t item = blockIdx.x * kStreamWarps + warp; item < items && ok; item += gridDim.x * kStreamWarps) {
@@ -99,13 +98,13 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
       }
     }
     __syncwarp();
-    // unit j into a slot, a lane for each box: panels of K, then of V
+    // unit j into a slot: the panels of K, then those of V, in one box
     auto issue = [&](uint32_t j, uint32_t to) {
-      if (j >= n_units) return;
-      const uint32_t b = smem_address(bar + to);
-      if (lane == 0) bar_expect(b, S::kUnitBytes);
-      __syncwarp();
-      if (lane < 2 * S::kPanels) tma_box(smem_address(ring + to * S::kUnitBytes + lane * S::kPanelBytes), &map, box_x, (int32_t)units[j].x + box_y, b);
+      if (j < n_units && lane == 0) {
+        const uint32_t b = smem_address(bar + to);
+        bar_expect(b, S::kUnitBytes);
+        tma_box(smem_address(ring + to * S::kUnitBytes), &map, 0, (int32_t)units[j].x, 0, b);
+      }
     };
 #pragma unroll
     for (int k = 0; k < S::kSlots; ++k) issue(k, slot + k < S::kSlots ? slot + k : slot + k - S::kSlots);
@@ -269,7 +268,7 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_ti
   using S = Stream<D>;
   const TableView& tv = a.tv;
   CUtensorMap map;
-  if (!block_map(tv, D, kUnit, &map)) return cudaErrorInvalidValue;
+  if (!block_map(tv, D, kUnit, D / 64, 2, &map)) return cudaErrorInvalidValue;
   const uint64_t np = prefix ? ((uint64_t)a.max_members * a.group + 15) / 16 * a.chunks[0] * tv.heads * a.n_groups : 0;
   const uint64_t ns = suffix ? (a.group + 15) / 16 * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
@@ -286,11 +285,12 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_ti
 
 bool has_block_map() { return encoder() != nullptr; }
 
-bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, CUtensorMap* map) {
+bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, uint32_t box_panels, uint32_t box_kv, CUtensorMap* map) {
   const Encode f = encoder();
-  const cuuint64_t dims[2] = {dk, tv.n * tv.n_chunks * tv.block_tokens}, strides[1] = {(cuuint64_t)dk * 2};
-  const cuuint32_t box[2] = {64, box_rows}, steps[2] = {1, 1};
-  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 2, tv.slab, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const uint64_t rows = tv.n * tv.n_chunks * tv.block_tokens, values = (uint64_t)(tv.n_chunks - 1u) * tv.heads * tv.block_tokens;
+  const cuuint64_t dims[4] = {64, rows - values, dk / 64, tv.n_chunks}, strides[3] = {(cuuint64_t)dk * 2, 128, values ? values * dk * 2 : 128};
+  const cuuint32_t box[4] = {64, box_rows, box_panels, box_kv}, steps[4] = {1, 1, 1, 1};
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT16, 4, tv.slab, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

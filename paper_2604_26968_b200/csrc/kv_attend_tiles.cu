@@ -156,7 +156,7 @@ __host__ __device__ constexpr int panel_at(int part, int p, int col0) {
 
 // The products of team r.  While the probabilities of tile t are formed, the scores of tile t + 1 are.
 template <typename T, typename S, int kCol0>
-__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int r_, uint32_t n_tiles_, bool shared_, uint32_t* status) {
+__device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_at, uint32_t ring_at, int r_, uint32_t n_tiles_, bool shared_, uint32_t box_rows_, uint32_t* status) {
   constexpr uint32_t kStage = S::kKBytes + S::kVBytes;
   constexpr uint32_t kScores = instruction<T>(S::kTok, false), kOutput = instruction<T>(S::kCols, true);
   volatile uint32_t* const gave_up = &ctl->gave_up;
@@ -183,11 +183,17 @@ __device__ __forceinline__ void issue(Control* ctl, uint32_t tmem_, uint32_t q_a
       }
     }
   };
+  // values: (MLA) panels of a tile, else panels of a block, blocks one after the other
+  const uint32_t box_rows = __shfl_sync(~0u, box_rows_, 0), v_panel = S::kLatent ? S::kPanelBytes : box_rows * 128u;
+  uint32_t v_step[S::kTok / 16];
+#pragma unroll
+  for (int k = 0; k < S::kTok / 16; ++k)
+    v_step[k] = S::kLatent ? k * 128u : (k * 16u / box_rows * (S::kBPanels * v_panel) + k * 16u % box_rows * 128u) / 16u;
   auto output = [&](uint32_t i, uint32_t t) {   // O_r += P_r[i & 1] V_t
-    const uint32_t v_op = operand(ring_at + (t % S::kStages) * kStage + S::kKBytes, S::kPanelBytes);
+    const uint32_t v_op = operand(ring_at + (t % S::kStages) * kStage + S::kKBytes, v_panel);
     const uint32_t p_at = tmem + S::kSAt + (2 * r + (i & 1)) * S::kTok;
 #pragma unroll
-    for (int k = 0; k < S::kTok / 16; ++k) mma_ts(o_at, p_at + k * 8, v_op + k * 128, kOutput, k ? 1u : i);
+    for (int k = 0; k < S::kTok / 16; ++k) mma_ts(o_at, p_at + k * 8, v_op + v_step[k], kOutput, k ? 1u : i);
   };
   auto wait = [&](unsigned long long* bar, uint32_t parity) {
     return __all_sync(~0u, bar_wait(smem_address(bar), parity, gave_up, status));
@@ -293,6 +299,7 @@ __device__ __forceinline__ void load_queries(const AttendArgs& a, const Item& w,
 
 template <typename T, typename S, bool kWeights>
 __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
+                                                               const __grid_constant__ CUtensorMap map_wide,
                                                                uint32_t first_kind_items, uint32_t box_rows, uint32_t outside,
                                                                uint32_t q_sign, uint32_t q_bits) {
   constexpr int kHalves = S::kDv / S::kCols;   // CTAs that share out a row tile's columns
@@ -355,7 +362,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     const int part = warp == 0 ? 0 : 1;
     const uint32_t bytes = part ? S::kVBytes : S::kKBytes, panels = part ? S::kBPanels : S::kAPanels;
-    const int32_t values = part && !S::kLatent ? (int32_t)(tv.heads * tv.block_tokens) : 0;
+    const int32_t kv = part && !S::kLatent ? 1 : 0;
     // boxes of a tile; the lanes look the blocks of 32 of them up at a time, before they are needed
     const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box, ahead = 32u / boxes;
     auto look = [&](uint32_t t) {   // of tiles t .. t + ahead - 1: the place of box lane % boxes of tile t + lane / boxes
@@ -394,11 +401,18 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
       }
       __syncwarp();
       const uint32_t dst = smem_address(ring) + st * (S::kKBytes + S::kVBytes) + (part ? S::kKBytes : 0);
-      for (uint32_t x0 = 0; x0 < boxes * panels; x0 += 32u) {      // a lane for each box of each panel
-        const uint32_t x = x0 + lane, p = x / boxes, box = x - p * boxes;
-        const uint32_t at = __shfl_sync(~0u, now, first + box);
-        if (x < boxes * panels)
-          tma_box(dst + p * S::kPanelBytes + box * rows_per_box * 128u, &map, panel_at<S>(part, p, col0), (int32_t)at + (at != outside ? values : 0), bar);
+      const uint32_t at = __shfl_sync(~0u, now, first + lane % boxes);      // (lane < boxes: its box's rows)
+      if (part && !S::kLatent) {             // values lie block by block, all panels of a block in one box
+        if ((uint32_t)lane < boxes) tma_box(dst + lane * rows_per_box * 128u * S::kBPanels, &map_wide, 0, (int32_t)at, 1, bar);
+      } else if (boxes == 1u) {              // a block (or more) is a tile: the panels in wide boxes, and (MLA) the last one of the scores'
+        if (lane == 0) tma_box(dst, &map_wide, panel_at<S>(part, 0, col0) / 64, (int32_t)at, kv, bar);
+        if (S::kLatent && part == 0 && lane == 0) tma_box(dst + (S::kAPanels - 1) * S::kPanelBytes, &map, S::kDk / 64 - 1, (int32_t)at, 0, bar);
+      } else {                               // a lane for each box of each panel
+        for (uint32_t x0 = 0; x0 < boxes * panels; x0 += 32u) {
+          const uint32_t x = x0 + lane, p = x / boxes, box = x - p * boxes;
+          const uint32_t y = __shfl_sync(~0u, now, first + box);
+          if (x < boxes * panels) tma_box(dst + p * S::kPanelBytes + box * rows_per_box * 128u, &map, panel_at<S>(part, p, col0) / 64, (int32_t)y, kv, bar);
+        }
       }
     }
   } else if (warp < S::kFirst) {
@@ -407,8 +421,8 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
     const int r = warp - 1;
     const uint32_t mine = shared ? (n_tiles + 1u - r) / 2u : n_tiles;
     if (r < teams && mine) {
-      if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, status);
-      else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, status);
+      if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, box_rows, status);
+      else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, box_rows, status);
     }
   } else {
     // ---- softmax: a thread per row ----
@@ -523,7 +537,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
           const uint32_t end = (left + box_rows - 1u) / box_rows * box_rows;
           for (uint32_t x = lane_at + lane; x < (end - left) * (S::kCols / 8u); x += 128u) {
             const uint32_t tok = left + x / (S::kCols / 8u), c = x % (S::kCols / 8u);
-            *reinterpret_cast<uint4*>(vt + (c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
+            const uint32_t to = S::kLatent ? c / 8u * S::kPanelBytes + tok * 128u
+                                           : (tok / box_rows * S::kBPanels + c / 8u) * box_rows * 128u + tok % box_rows * 128u;
+            *reinterpret_cast<uint4*>(vt + to + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
           }
           proxy_fence();
         }
@@ -600,8 +616,8 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s
   const TableView& tv = a.tv;
   const uint32_t box = tv.block_tokens < (uint32_t)S::kTok ? tv.block_tokens : (uint32_t)S::kTok;
   const uint64_t rows = tv.n * tv.n_chunks * tv.block_tokens;
-  CUtensorMap map;
-  if (!block_map(tv, S::kDk, box, &map)) return cudaErrorInvalidValue;
+  CUtensorMap map, map_wide;
+  if (!block_map(tv, S::kDk, box, 1, 1, &map) || !block_map(tv, S::kDk, box, S::kBPanels, 1, &map_wide)) return cudaErrorInvalidValue;
   const uint64_t tile = S::kTiles * 128;
   const uint64_t np = prefix ? ((uint64_t)a.max_members * a.group + tile - 1) / tile * a.chunks[0] * tv.heads * a.n_groups : 0;
   const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
@@ -622,7 +638,7 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s
     b.scale2 = 1.0f;
     bits = 0;
   }
-  return launch_overlapped_smem(kernel, (unsigned)grid, (unsigned)S::kThreads, S::kSmem, s, b, map, (uint32_t)np, box, (uint32_t)rows, sign, bits);
+  return launch_overlapped_smem(kernel, (unsigned)grid, (unsigned)S::kThreads, S::kSmem, s, b, map, map_wide, (uint32_t)np, box, (uint32_t)rows, sign, bits);
 }
 
 using Heads128 = Shape<128, 128, 128, 2, 64, 4>;
@@ -637,11 +653,10 @@ cudaError_t launch_typed(const AttendArgs& a, bool mla, bool prefix, bool suffix
 
 }  // namespace
 
-bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows, bool weights) {
+bool tiles_take(uint32_t dk, uint32_t dv, bool mla, uint32_t block_tokens, uint64_t slab_rows) {
   const uint32_t tok = mla ? Latents::kTok : Heads128::kTok;
   if (mla ? dk != 576 || dv != 512 : dk != 128 && dk != 64) return false;
-  if (block_tokens % 8 != 0 || (tok % block_tokens != 0 && block_tokens % tok != 0)) return false;
-  if (weights && block_tokens % 16 != 0) return false;   // (they are kept by 16 tokens)
+  if (block_tokens % 16 != 0 || (tok % block_tokens != 0 && block_tokens % tok != 0)) return false;
   // (a box's place is a signed number of rows)
   return slab_rows < 0x7fff0000ull && has_block_map();
 }

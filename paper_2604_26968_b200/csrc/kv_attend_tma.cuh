@@ -54,17 +54,21 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   atomicOr(status, KV_DEV_WAIT_EXPIRED);
   return false;
 }
-__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, uint32_t bar) {
+// What the thread has written to shared memory comes before what copies and products do with it.
+__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// A box from row y and panel (64 elements) x on; kv: the chunk of keys, or the one of values.
+__device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t kv, uint32_t bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(0), "r"(y), "r"(x), "r"(kv), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// The tensor map of a partition's slab: rows of `dk` elements, boxes of box_rows rows x 64 elements (128 bytes, with the
-// 128-byte swizzle).  False: the driver refuses it.
-bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, CUtensorMap* map);
+// Tensor map of a partition's slab as [K, V][panel][row][64 elements], rows of dk elements; a box is box_rows rows of
+// box_panels panels of box_kv chunks, panel by panel, each a row of 128 bytes with the 128-byte swizzle.  A box costs the copy
+// engine about 60 cycles and 4 more for each of its 128-byte rows (measured), so boxes are as large as
+// blocks and layouts let them be.  False: the driver refuses the map.
+bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, uint32_t box_panels, uint32_t box_kv, CUtensorMap* map);
 bool has_block_map();
 
 }  // namespace kvt

@@ -110,7 +110,7 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
   const uint64_t prefix_rows = (uint64_t)max_members * group;
   const uint64_t slab_rows = v.geom[q].n * v.geom[q].n_chunks * bt;
   const bool streams = stream_takes(dk, dv, mla, bt, slab_rows);
-  const bool fits = tiles_take(dk, dv, mla, bt, slab_rows, weights);
+  const bool fits = tiles_take(dk, dv, mla, bt, slab_rows);
   uint64_t limit = (uint64_t)kMaxChunkBlocks * bt / 64 * 64;   // most tokens of a chunk
   if (limit < 64) limit = 64;
   if (limit > kMaxChunkTokens) limit = kMaxChunkTokens;

@@ -324,3 +324,96 @@ def test_no_sequences_and_refusals():
         p.kv_attend(0, 1, q, out.half(), table, suffix, **call)
     p.sync()
     c.close()
+
+
+@pytest.mark.parametrize("shape,members,plen,block", [("gqa", 64, 9_000, 16), ("gqa", 20, 5_000, 32), ("gqa64", 70, 6_001, 16), ("mqa", 3, 4_000, 64),
+                                                      ("mla", 6, 3_000, 64), ("mla", 3, 1_500, 16), ("gqa", 4, 7_000, 16)])
+def test_long_runs_give_the_same_bits_every_time(shape, members, plen, block):
+    """Many tiles and chunks on all SMs: ten calls, scratch filled with NaN before each."""
+    c = cache(shape, block, plen // block + 150)
+    S = members + 1
+    suffix, rows = runs([(53 * i) % 300 for i in range(S)], block)
+    prefix, rows = runs([plen], block, rows)
+    table, q = c.table(rows), queries(c, S)
+    want = c.expect(q, table, suffix, prefix, [0, members])
+    first = None
+    for _ in range(10):
+        w = torch.zeros(c.pool.n_tags, dtype=torch.int64, device="cuda")
+        got = (*c.attend(q, table, suffix, prefix, [0, members], weight=w), w)
+        if first is None:
+            c.compare(got[0], got[1], want)
+            first = got
+        for x, y in zip(first, got):
+            assert torch.equal(x, y)
+    assert c.pool.kv_device_status() == 0
+    c.close()
+
+
+@pytest.mark.parametrize("shape", ["gqa", "gqa64", "mqa71", "mla"])
+def test_groups_of_many_and_few_members(shape):
+    """One launch for groups on both sides of a row tile; a group of none; prefixes of nothing, one token, many."""
+    c = cache(shape, 16, 420)
+    sizes = [1, 40, 0, 3, 20, 5]
+    starts = [sum(sizes[:i]) for i in range(len(sizes) + 1)]
+    S = starts[-1] + 2
+    suffix, rows = runs([(29 * i) % 70 for i in range(S)], 16)
+    prefix, rows = runs([700, 1_111, 5, 0, 64, 1], 16, rows)
+    check(c, queries(c, S), c.table(rows), suffix, prefix, starts, weights=True)
+    c.close()
+
+
+@pytest.mark.parametrize("scale", [-0.11, 0.0, 1e-3, 3.0])
+@pytest.mark.parametrize("shape,members", [("gqa", 3), ("gqa", 12), ("odd80", 3), ("mla", 2)])
+def test_scales(shape, members, scale):
+    c = cache(shape, 16, 90)
+    suffix, rows = runs([70, 0, 33] + [5] * members, 16)
+    prefix, rows = runs([321], 16, rows)
+    table, q = c.table(rows), queries(c, members + 3, by=0.5)
+    table[2, c.layer, 0] = NONE
+    want = c.expect(q, table, suffix, prefix, [0, members], scale=scale)
+    out, lse = c.attend(q, table, suffix, prefix, [0, members], scale=scale)
+    c.compare(out, lse, want)
+    c.close()
+
+
+def test_two_streams_at_once():
+    """Two calls on two streams, each with its own scratch, while the other runs."""
+    c = cache("gqa", 16, 500)
+    suffix, rows = runs([300] * 12, 16)
+    prefix, rows = runs([3_000], 16, rows)
+    table = c.table(rows)
+    work = []
+    for i in range(2):
+        q = queries(c, 12)
+        want = c.expect(q, table, suffix, prefix, [0, 10 + i])
+        b = dict(max_suffix=300, max_prefix=3_000, max_members=11)
+        work.append(dict(q=q, want=want, out=torch.empty((12, 32, 128), dtype=c.dtype, device="cuda"), lse=torch.empty((12, 32), device="cuda"),
+                         scratch=c.scratch(12, 1, **b), stream=torch.cuda.Stream(), group=torch.tensor([0, 10 + i], dtype=torch.int32, device="cuda"), b=b))
+    d_s = torch.tensor(suffix, dtype=torch.int32, device="cuda")
+    d_p = torch.tensor(prefix, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for w in work:
+            assert c.pool.kv_attend(0, 1, w["q"], w["out"], table, d_s, scale=128 ** -0.5, d_scratch=w["scratch"], d_prefix=d_p, d_group=w["group"],
+                                    d_lse=w["lse"], stream=w["stream"], **w["b"]) == 0
+    torch.cuda.synchronize()
+    for w in work:
+        c.compare(w["out"], w["lse"], w["want"])
+    c.close()
+
+
+def test_infinite_and_nan_queries_stay_in_their_rows():
+    c = cache("gqa", 16, 120)
+    suffix, rows = runs([64] * 20, 16)
+    prefix, rows = runs([500], 16, rows)
+    table, q = c.table(rows), queries(c, 20)
+    want = c.expect(q, table, suffix, prefix, [0, 18])
+    q[3, 5] = math.nan
+    q[19, 7] = math.inf
+    out, lse = c.attend(q, table, suffix, prefix, [0, 18])
+    keep = torch.ones((20, 32), dtype=torch.bool, device="cuda")
+    keep[3, 5] = keep[19, 7] = False
+    assert bool(out[3, 5].isnan().all()) and bool(lse[3, 5].isnan())
+    out, lse = torch.where(keep[..., None], out, want[0].to(c.dtype)), torch.where(keep, lse, want[1].float())
+    c.compare(out, lse, want)
+    c.close()

@@ -330,7 +330,7 @@ def test_no_sequences_and_refusals():
                                                       ("mla", 6, 3_000, 64), ("mla", 3, 1_500, 16), ("gqa", 4, 7_000, 16)])
 def test_long_runs_give_the_same_bits_every_time(shape, members, plen, block):
     """Many tiles and chunks on all SMs: ten calls, scratch filled with NaN before each."""
-    c = cache(shape, block, plen // block + 150)
+    c = cache(shape, block, plen // block + 20 * members + 50)
     S = members + 1
     suffix, rows = runs([(53 * i) % 300 for i in range(S)], block)
     prefix, rows = runs([plen], block, rows)

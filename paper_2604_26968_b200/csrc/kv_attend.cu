@@ -568,33 +568,32 @@ __global__ void __launch_bounds__(kFinishThreads) finish_kernel(const __grid_con
 }
 
 // Weight of the blocks of prefixes (the first prefix_ctas CTAs) and suffixes: the sum over a block's rows of what the kernels have
-// left for its grains, taken from the rows' sums; `lanes` threads for a block and kWeightRows of its rows.
-__global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_constant__ AttendArgs a, uint32_t prefix_ctas, uint32_t prefix_lanes,
-                                                               uint32_t suffix_lanes) {
+// left for its grains, taken from the rows' sums; 2^shift threads for a block and kWeightRows of its rows.
+__global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_constant__ AttendArgs a, uint32_t prefix_ctas, uint32_t prefix_shift,
+                                                               uint32_t suffix_shift) {
   const int kind = blockIdx.x < prefix_ctas ? kKindPrefix : kKindSuffix;
-  const uint32_t lanes = kind == kKindPrefix ? prefix_lanes : suffix_lanes;
-  const uint64_t item = ((uint64_t)(blockIdx.x - (kind == kKindPrefix ? 0u : prefix_ctas)) * kFinishThreads + threadIdx.x) / lanes;
-  const uint32_t lane = threadIdx.x % lanes;
+  const uint32_t shift = kind == kKindPrefix ? prefix_shift : suffix_shift, lanes = 1u << shift;
+  // (fewer than 2^32 items, see the launch: 64-bit divisions were most of this kernel's time)
+  const uint32_t item = (blockIdx.x - (kind == kKindPrefix ? 0u : prefix_ctas)) * (kFinishThreads >> shift) + (threadIdx.x >> shift);
+  const uint32_t lane = threadIdx.x & (lanes - 1u);
   const uint32_t most_blocks = ((kind == kKindPrefix ? a.max_prefix : a.max_suffix) + a.tv.block_tokens - 1u) / a.tv.block_tokens;
   const uint32_t most_rows = kind == kKindPrefix ? a.max_members * a.group : a.group, shares = (most_rows + kWeightRows - 1u) / kWeightRows;
-  const uint64_t sb = item / shares, sh = sb / most_blocks;
-  const uint32_t row0 = (uint32_t)(item - sb * shares) * kWeightRows, b = (uint32_t)(sb - sh * most_blocks);
-  const uint64_t index = sh / a.tv.heads;
-  const uint32_t head = (uint32_t)(sh - index * a.tv.heads);
+  const uint32_t sb = item / shares, sh = sb / most_blocks, index = sh / a.tv.heads;
+  const uint32_t row0 = (item - sb * shares) * kWeightRows, b = sb - sh * most_blocks, head = sh - index * a.tv.heads;
   unsigned long long w = 0;
   uint32_t handle = KV_NONE;
   if (index < (kind == kKindPrefix ? a.n_groups : a.n_seqs)) {
-    uint32_t seq0 = (uint32_t)index, rows = a.group, stride = a.group;
+    uint32_t seq0 = index, rows = a.group, stride = a.group;
     Segment seg;
     if (kind == kKindPrefix) {
       uint32_t lo, hi;
-      a.members((uint32_t)index, lo, hi, false);
+      a.members(index, lo, hi, false);
       seq0 = lo;
       rows = (hi - lo) * a.group;
       stride = a.max_members * a.group;
-      seg = a.checked(a.prefix, (uint32_t)index, a.max_prefix, false);
+      seg = a.checked(a.prefix, index, a.max_prefix, false);
     } else {
-      seg = a.checked(a.suffix, (uint32_t)index, a.max_suffix, false);
+      seg = a.checked(a.suffix, index, a.max_suffix, false);
     }
     const uint32_t from = b * a.tv.block_tokens;
     const uint64_t at = (uint64_t)seg.row + b;
@@ -606,11 +605,11 @@ __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_con
       const uint32_t to = min(seg.tokens, from + a.tv.block_tokens);
       const uint32_t g0 = from / a.grain_tokens, g1 = (to + a.grain_tokens - 1u) / a.grain_tokens;
       const float* const total = a.direct ? a.part_lse : a.total;
-      const float* const grain = a.grain[kind] + (index * a.tv.heads + head) * (uint64_t)a.grains[kind] * stride;
+      const float* const grain = a.grain[kind] + (uint64_t)sh * a.grains[kind] * stride;
       float sum = 0.0f;
 #pragma unroll 4
       for (uint32_t r = row0 + lane; r < rows; r += lanes) {
-        const uint32_t member = r / a.group;
+        const uint32_t member = a.by_group(r);
         const float lse = total[(uint64_t)(seq0 + member) * a.q_heads + head * a.group + (r - member * a.group)];
         if (lse == -INFINITY) continue;
         for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r] - lse);
@@ -695,17 +694,19 @@ cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t 
   }
   if (!a.weight) return cudaSuccess;
   uint64_t ctas[2] = {0, 0};
-  uint32_t lanes[2] = {1, 1};
+  uint32_t shift[2] = {0, 0};
   for (int kind = prefix ? 0 : 1; kind < 2; ++kind) {
     const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
     const uint64_t blocks = ((uint64_t)most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
     const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
-    while (lanes[kind] < 32u && lanes[kind] < r) lanes[kind] *= 2u;
-    ctas[kind] = ((uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks * ((r + kWeightRows - 1u) / kWeightRows) * lanes[kind] + kFinishThreads - 1) / kFinishThreads;
+    while (shift[kind] < 5u && (1u << shift[kind]) < r) ++shift[kind];
+    const uint64_t items = (uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks * ((r + kWeightRows - 1u) / kWeightRows);
+    if (items > 0xf0000000ull) return cudaErrorInvalidValue;
+    ctas[kind] = ((items << shift[kind]) + kFinishThreads - 1) / kFinishThreads;
   }
   if (ctas[0] + ctas[1] == 0) return cudaSuccess;
   if (ctas[0] + ctas[1] > 0x7fffffffull) return cudaErrorInvalidValue;
-  return launch_overlapped(weight_kernel, (unsigned)(ctas[0] + ctas[1]), (unsigned)kFinishThreads, s, a, (uint32_t)ctas[0], lanes[0], lanes[1]);
+  return launch_overlapped(weight_kernel, (unsigned)(ctas[0] + ctas[1]), (unsigned)kFinishThreads, s, a, (uint32_t)ctas[0], shift[0], shift[1]);
 }
 
 }  // namespace

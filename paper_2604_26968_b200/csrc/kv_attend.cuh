@@ -68,6 +68,7 @@ struct AttendArgs {
   int64_t q_seq, q_head, out_seq, out_head;   // strides in elements
   float scale2;                               // scale * log2(e)
   uint32_t n_seqs, n_groups, q_heads, group;  // group: query heads of a KV head
+  Divisor by_group;
   uint32_t dk, dv;                            // elements of a key row and of a value row
   const uint32_t* suffix;                     // [n_seqs][2]
   const uint32_t* prefix;                     // [n_groups][2]

@@ -94,7 +94,7 @@ __device__ __forceinline__ bool item_of(const AttendArgs& a, int kind, uint32_t 
 
 // Row r of an item: its sequence and query head.
 __device__ __forceinline__ void row_of(const AttendArgs& a, const Item& w, uint32_t r, uint32_t& seq, uint32_t& head) {
-  const uint32_t at = w.row0 + r, member = at / a.group;
+  const uint32_t at = w.row0 + r, member = a.by_group(at);
   seq = w.seq0 + member;
   head = w.head * a.group + (at - member * a.group);
 }

@@ -224,6 +224,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   a.n_groups = sp.chunks[0] ? d->n_groups : 0u;
   a.q_heads = (uint32_t)v.desc->part[q].model.n_q_heads;
   a.group = a.q_heads / a.tv.heads;
+  a.by_group = Divisor(a.group);
   a.dk = dk;
   a.dv = dv;
   a.suffix = d->d_suffix;

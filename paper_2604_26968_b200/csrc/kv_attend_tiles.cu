@@ -6,17 +6,23 @@
 // of tokens lies in shared memory as the matrix instructions want it whatever blocks it is made of; a block
 // that is not there is a box outside the tensor, which reads as zeros.
 //
-// Roles: warps 0 and 3 look blocks up and issue the copies, a warp for each row tile issues its matrix
-// instructions, and each further group of four warps is a row tile's softmax, a thread per row: it reads its row
+// Roles: warps 0 and 3 look blocks up and issue the copies of keys and of values, warps 1 and 2 issue the matrix instructions of
+// a team each, and each further group of four warps is a team's softmax, a thread per row: it reads its row
 // of S, keeps maximum and sum, and writes the probabilities over S, from where P V takes them as the operand
-// in tensor memory.  With two row tiles (kTiles == 2) the tensor cores work on one's products while the
-// other's probabilities are formed; with one (kTiles == 1, MLA) S has two places and the scores of
-// the next tokens are formed meanwhile.  The output is rescaled only when a row's maximum has grown by
-// more than 2^8 since the last time (its sum is kept to the same base, so that results are what they were).
+// in tensor memory.  A team has a row tile, or, where one is all there can be, every other tile of its tokens.  S has two
+// places a team, so that the scores of the next tokens are formed while these become probabilities.
+// The output is rescaled only when a row's maximum has grown by more than 2^8 since the last time (its sum is kept to the same
+// base, so that results are what they were).
 //
 // MLA: a row of 576 elements is key (all of them) and value (the first 512).  128 x 512 outputs would
 // fill the tensor memory, so a CTA takes 256 of the columns, and both CTAs form the scores.  The first 256 elements
 // of Q lie in tensor memory, which leaves room for two tiles of 64 tokens in shared memory.
+//
+// Measured: 64 tokens by two row tiles of 128-element heads take about 2,000 cycles of an SM: exponentials 1,024 at the
+// least, products about 1,200, the softmax of either team 1,500 to 1,800 (half of it latencies: waits, reads of tensor memory,
+// the maximum), so the chain of a team from scores to probabilities to output bounds it.  64 tokens by 128 MLA rows and half the
+// columns: 1,830 cycles on a few SMs, 2,800 on all of them (the L2 is a seventh busy then, the tensor pipe 41 %; what makes
+// the difference is not established).  Of the measured matrix rate whole calls reach 0.38 and 0.28.
 //
 // Every wait is bounded: one that gives up sets KV_DEV_WAIT_EXPIRED and a flag that ends the other
 // waits; copies and matrix instructions in flight are then waited for (bounded) before the CTA leaves.
@@ -611,6 +617,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   }
 }
 
+template <typename F>
+int registers_of(F* kernel) {
+  cudaFuncAttributes f{};
+  return cudaFuncGetAttributes(&f, kernel) == cudaSuccess ? f.numRegs : 0;
+}
+
 template <typename T, typename S>
 cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s) {
   const TableView& tv = a.tv;
@@ -625,6 +637,12 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s
   if (grid == 0) return cudaSuccess;
   if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
   auto* kernel = a.weight ? tiles_kernel<T, S, true> : tiles_kernel<T, S, false>;
+  if (S::kTiles == 2) {
+    // (the softmax's warps take up registers that the launch has to have given the CTA: fewer, and they would wait for good)
+    static const bool enough[2] = {registers_of(tiles_kernel<T, S, false>) * S::kThreads >= 128 * (72 + 2 * 216),
+                                   registers_of(tiles_kernel<T, S, true>) * S::kThreads >= 128 * (72 + 2 * 216)};
+    if (!enough[a.weight ? 1 : 0]) return cudaErrorInvalidConfiguration;
+  }
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;
   AttendArgs b = a;

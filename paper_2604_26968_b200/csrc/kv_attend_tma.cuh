@@ -65,9 +65,9 @@ __device__ __forceinline__ void tma_box(uint32_t dst, const CUtensorMap* map, in
 }
 
 // Tensor map of a partition's slab as [K, V][panel][row][64 elements], rows of dk elements; a box is box_rows rows of
-// box_panels panels of box_kv chunks, panel by panel, each a row of 128 bytes with the 128-byte swizzle.  A box costs the copy
-// engine about 60 cycles and 4 more for each of its 128-byte rows (measured), so boxes are as large as
-// blocks and layouts let them be.  False: the driver refuses the map.
+// box_panels panels of box_kv chunks, panel by panel, each a row of 128 bytes with the 128-byte swizzle.  Boxes are as large as
+// blocks and layouts let them be (one for a unit of 16 tokens instead of four: 64 chats 74 -> 71 us).
+// False: the driver refuses the map.
 bool block_map(const TableView& tv, uint32_t dk, uint32_t box_rows, uint32_t box_panels, uint32_t box_kv, CUtensorMap* map);
 bool has_block_map();
 

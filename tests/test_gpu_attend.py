@@ -11,7 +11,7 @@ from paper_2604_26968_b200 import binding as B
 pytestmark = pytest.mark.gpu
 
 SHAPES = {"gqa64": ("gqa", 16, 4, 64, 0), "gqa": ("gqa", 32, 8, 128, 0), "gqa8": ("gqa", 16, 2, 128, 0), "mha": ("mha", 6, 6, 128, 0),
-          "mqa": ("mqa", 32, 1, 128, 0), "mqa71": ("mqa", 71, 1, 64, 0), "wide": ("gqa", 8, 2, 256, 0), "odd80": ("gqa", 6, 2, 80, 0),
+          "mqa": ("mqa", 32, 1, 128, 0), "mqa71": ("mqa", 71, 1, 64, 0), "mqa160": ("mqa", 160, 1, 128, 0), "wide": ("gqa", 8, 2, 256, 0), "odd80": ("gqa", 6, 2, 80, 0),
           "odd8": ("gqa", 3, 3, 8, 0), "mla": ("mla", 128, 1, 512, 64), "mla16": ("mla", 16, 1, 512, 64), "mla_small": ("mla", 5, 1, 64, 16)}
 DT = {"bf16": torch.bfloat16, "fp16": torch.float16}
 
@@ -62,7 +62,7 @@ def test_suffixes_of_many_lengths(shape, dtype):
 
 
 @pytest.mark.parametrize("length", [0, 1, 77, 128, 129])
-@pytest.mark.parametrize("shape", ["gqa64", "gqa", "mqa", "mla"])
+@pytest.mark.parametrize("shape", ["gqa64", "gqa", "mqa", "mqa160", "mla"])
 def test_one_sequence(shape, length):
     c = cache(shape, 16, 32)
     suffix, rows = runs([length], 16)

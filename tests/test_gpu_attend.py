@@ -417,3 +417,22 @@ def test_infinite_and_nan_queries_stay_in_their_rows():
     out, lse = torch.where(keep[..., None], out, want[0].to(c.dtype)), torch.where(keep, lse, want[1].float())
     c.compare(out, lse, want)
     c.close()
+
+
+@pytest.mark.parametrize("block", [16, 32, 48, 64, 96, 128, 256])
+@pytest.mark.parametrize("shape,members", [("gqa", 11), ("gqa64", 40), ("mqa160", 1), ("mla", 2)])
+def test_tiles_of_any_block_size(shape, members, block):
+    """Runs that end inside a tile, a block, a block longer than a tile; garbage behind their last token."""
+    c = cache(shape, block, 3_000 // block + 4 * members + 30)
+    S = members + 2
+    suffix, rows = runs([(block * i + 7 * i + 1) % 200 for i in range(S)], block)
+    prefix, rows = runs([2 * block + 1_017, 65], block, rows)
+    table = c.table(rows)
+    for row, n in suffix + prefix:
+        if n % block:
+            for h in range(c.H):
+                e = int(c.entry(table[row + n // block, c.layer, h]))
+                c.slab[e // c.H, :, e % c.H, n % block:] = math.nan
+    table[1, c.layer, 0] = NONE
+    check(c, queries(c, S), table, suffix, prefix, [0, members, members + 1], weights=True)
+    c.close()

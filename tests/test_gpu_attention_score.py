@@ -170,3 +170,50 @@ def test_append_attend_evict_and_promote():
         step(n_new + 1)
         assert p.kv_device_status() == 0
     c.close()
+
+
+def test_a_captured_step_replayed():
+    """Tokens in, attention with weights, score and victims in one graph: its replays do what the calls do."""
+    part = partition("gqa", 32, 8, 128, 0, 16, 60, ring=64)
+    S, n = 5, 9
+    inv = (10_000.0 ** (-torch.arange(64, device="cuda", dtype=torch.float64) / 64)).float()
+    rope = B.kv_rope(128, [0] * 20 + [1] * 22 + [2] * 22, inv)
+
+    def world():
+        c = Cache(part, torch.bfloat16, seed=3)
+        g = c.gen
+        r = lambda *x: torch.randn(x, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+        table = c.table(40)
+        w = dict(c=c, table=table, k=r(n, 8, 128), v=r(n, 8, 128), q=r(n, 32, 128), slot=torch.arange(3, 3 + n, device="cuda"),
+                 pos=torch.arange(3 * n, dtype=torch.int32, device="cuda").view(3, n), qs=r(S, 32, 128), out=torch.zeros(S, 32, 128, dtype=torch.bfloat16, device="cuda"),
+                 lse=torch.zeros(S, 32, device="cuda"), suffix=torch.tensor([(30 + s, 3 * s) for s in range(S)], dtype=torch.int32, device="cuda"),
+                 prefix=torch.tensor([(0, 400)], dtype=torch.int32, device="cuda"), group=torch.tensor([0, 4], dtype=torch.int32, device="cuda"),
+                 weight=torch.zeros(c.pool.n_tags, dtype=torch.int64, device="cuda"), acc=torch.zeros(c.pool.n_tags, device="cuda"),
+                 victims=torch.zeros(100, dtype=torch.int32, device="cuda"), scratch=c.scratch(S, 1, max_suffix=20, max_prefix=500, max_members=5, weights=True))
+        torch.cuda.synchronize()
+        return w
+
+    def step(w):
+        p = w["c"].pool
+        assert p.kv_append(0, 1, w["k"], w["v"], w["table"], w["slot"], d_q=w["q"], d_q_out=w["q"], rope=rope, d_pos=w["pos"]) == 0
+        assert p.kv_attend(0, 1, w["qs"], w["out"], w["table"], w["suffix"], max_suffix=20, scale=0.09, d_scratch=w["scratch"], d_prefix=w["prefix"],
+                           d_group=w["group"], max_prefix=500, max_members=5, d_lse=w["lse"], d_weight=w["weight"]) == 0
+        assert p.kv_attention_score(7, 0.5, 1, w["weight"], w["acc"]) == 0
+        assert p.kv_select_victims(100, w["victims"]) == 0
+
+    a, b = world(), world()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=b["c"].pool.compute):
+        step(b)
+    for _ in range(3):
+        step(a)
+        a["c"].pool.sync()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x in ("q", "out", "lse", "weight", "acc", "victims"):
+            assert torch.equal(a[x], b[x]), x
+        assert torch.equal(a["c"].slab.view(torch.int16), b["c"].slab.view(torch.int16))
+        assert torch.equal(a["c"].pool.score, b["c"].pool.score)
+    del graph
+    a["c"].close()
+    b["c"].close()

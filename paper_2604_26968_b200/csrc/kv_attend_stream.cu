@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(kStreamWarps * 32, Stream<D>::kCtas)
           const uint32_t tok = left + x / (S::kPanels * 8u), c = x % (S::kPanels * 8u);
           *reinterpret_cast<uint4*>(unit + (S::kPanels + c / 8u) * S::kPanelBytes + tok * 128u + (c % 8u) * 16u) = make_uint4(0, 0, 0, 0);
         }
+        proxy_fence();      // (the warp's next chunk has its first units copied into this slot: behind these zeros)
         __syncwarp();
       }
       // scores, the even and the odd steps of the sum on their own

@@ -363,76 +363,79 @@ __global__ void __launch_bounds__(S::kThreads, 1) tiles_kernel(const __grid_cons
   volatile uint32_t* const gave_up = &ctl->gave_up;
   uint32_t* const status = tv.status;
 
-  if (warp == 0 || warp == 3) {
-    // ---- blocks: a warp for each part of the stages ----
-    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    const int part = warp == 0 ? 0 : 1;
-    const uint32_t bytes = part ? S::kVBytes : S::kKBytes, panels = part ? S::kBPanels : S::kAPanels;
-    const int32_t kv = part && !S::kLatent ? 1 : 0;
-    // boxes of a tile; the lanes look the blocks of 32 of them up at a time, before they are needed
-    const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box, ahead = 32u / boxes;
-    auto look = [&](uint32_t t) {   // of tiles t .. t + ahead - 1: the place of box lane % boxes of tile t + lane / boxes
-      const uint32_t at = w.from + (t * boxes + lane) * rows_per_box;
-      if ((uint32_t)lane >= boxes * ahead || at >= w.to) return outside;
-      const uint32_t b = tv.by_tokens(at), ch = tv.chunk((uint64_t)w.seg.row + b, w.head);
-      return ch == ~0u ? outside : ch * tv.block_tokens + at - b * tv.block_tokens;
-    };
-    uint32_t next = look(0), now = outside;
-    bool ok = true;
-    for (uint32_t t = 0; t < n_tiles && ok; ++t) {
-      const uint32_t st = t % S::kStages, round = t / S::kStages;
-      if (t % ahead == 0) {
-        now = next;
-        if (t + ahead < n_tiles) next = look(t + ahead);
-      }
-      const uint32_t first = t % ahead * boxes, tile0 = w.from + t * S::kTok;
-      uint32_t bits[S::kTok / 32];
-      if (part == 0) {
-#pragma unroll
-        for (int m = 0; m < S::kTok / 32; ++m) {
-          const uint32_t tok = m * 32 + lane;
-          bits[m] = __ballot_sync(~0u, __shfl_sync(~0u, now, first + tok / rows_per_box) != outside && tile0 + tok < w.to);
+  if (warp < S::kFirst) {
+    // (one instruction for the four warps of the warpgroup, whatever their roles; 72 registers and 216 for the softmax make their
+    // code spill: a document's prefix and suffixes 117 us, these 114)
+    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+    if (warp == 0 || warp == 3) {
+      // ---- blocks: a warp for each part of the stages ----
+      const int part = warp == 0 ? 0 : 1;
+      const uint32_t bytes = part ? S::kVBytes : S::kKBytes, panels = part ? S::kBPanels : S::kAPanels;
+      const int32_t kv = part && !S::kLatent ? 1 : 0;
+      // boxes of a tile; the lanes look the blocks of 32 of them up at a time, before they are needed
+      const uint32_t rows_per_box = box_rows, boxes = S::kTok / rows_per_box, ahead = 32u / boxes;
+      auto look = [&](uint32_t t) {   // of tiles t .. t + ahead - 1: the place of box lane % boxes of tile t + lane / boxes
+        const uint32_t at = w.from + (t * boxes + lane) * rows_per_box;
+        if ((uint32_t)lane >= boxes * ahead || at >= w.to) return outside;
+        const uint32_t b = tv.by_tokens(at), ch = tv.chunk((uint64_t)w.seg.row + b, w.head);
+        return ch == ~0u ? outside : ch * tv.block_tokens + at - b * tv.block_tokens;
+      };
+      uint32_t next = look(0), now = outside;
+      bool ok = true;
+      for (uint32_t t = 0; t < n_tiles && ok; ++t) {
+        const uint32_t st = t % S::kStages, round = t / S::kStages;
+        if (t % ahead == 0) {
+          now = next;
+          if (t + ahead < n_tiles) next = look(t + ahead);
+        }
+        const uint32_t first = t % ahead * boxes, tile0 = w.from + t * S::kTok;
+        uint32_t bits[S::kTok / 32];
+        if (part == 0) {
+  #pragma unroll
+          for (int m = 0; m < S::kTok / 32; ++m) {
+            const uint32_t tok = m * 32 + lane;
+            bits[m] = __ballot_sync(~0u, __shfl_sync(~0u, now, first + tok / rows_per_box) != outside && tile0 + tok < w.to);
+          }
+        }
+        if (round) ok = bar_wait(smem_address(part ? &ctl->v_empty[st] : &ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
+        ok = __all_sync(~0u, ok);
+        if (!ok) break;
+        const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
+        if (lane == 0) {
+          if (part == 0) {   // (ahead of the copies that the scores wait for)
+  #pragma unroll
+            for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
+          }
+          bar_expect(bar, bytes);
+        }
+        __syncwarp();
+        const uint32_t dst = smem_address(ring) + st * (S::kKBytes + S::kVBytes) + (part ? S::kKBytes : 0);
+        const uint32_t at = __shfl_sync(~0u, now, first + lane % boxes);      // (lane < boxes: its box's rows)
+        if (part && !S::kLatent) {             // values lie block by block, all panels of a block in one box
+          if ((uint32_t)lane < boxes) tma_box(dst + lane * rows_per_box * 128u * S::kBPanels, &map_wide, 0, (int32_t)at, 1, bar);
+        } else if (boxes == 1u) {              // a block (or more) is a tile: the panels in wide boxes, and (MLA) the last one of the scores'
+          if (lane == 0) tma_box(dst, &map_wide, panel_at<S>(part, 0, col0) / 64, (int32_t)at, kv, bar);
+          if (S::kLatent && part == 0 && lane == 0) tma_box(dst + (S::kAPanels - 1) * S::kPanelBytes, &map, S::kDk / 64 - 1, (int32_t)at, 0, bar);
+        } else {                               // a lane for each box of each panel
+          for (uint32_t x0 = 0; x0 < boxes * panels; x0 += 32u) {
+            const uint32_t x = x0 + lane, p = x / boxes, box = x - p * boxes;
+            const uint32_t y = __shfl_sync(~0u, now, first + box);
+            if (x < boxes * panels) tma_box(dst + p * S::kPanelBytes + box * rows_per_box * 128u, &map, panel_at<S>(part, p, col0) / 64, (int32_t)y, kv, bar);
+          }
         }
       }
-      if (round) ok = bar_wait(smem_address(part ? &ctl->v_empty[st] : &ctl->k_empty[st]), (round - 1) & 1, gave_up, status);
-      ok = __all_sync(~0u, ok);
-      if (!ok) break;
-      const uint32_t bar = smem_address(part ? &ctl->v_full[st] : &ctl->k_full[st]);
-      if (lane == 0) {
-        if (part == 0) {   // (ahead of the copies that the scores wait for)
-#pragma unroll
-          for (int m = 0; m < S::kTok / 32; ++m) ctl->mask[t % S::kMasks][m] = bits[m];
-        }
-        bar_expect(bar, bytes);
+    } else {
+      // ---- matrix instructions: a warp for each row tile; the whole warp waits, one thread issues ----
+      const int r = warp - 1;
+      const uint32_t mine = shared ? (n_tiles + 1u - r) / 2u : n_tiles;
+      if (r < teams && mine) {
+        if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, box_rows, status);
+        else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, box_rows, status);
       }
-      __syncwarp();
-      const uint32_t dst = smem_address(ring) + st * (S::kKBytes + S::kVBytes) + (part ? S::kKBytes : 0);
-      const uint32_t at = __shfl_sync(~0u, now, first + lane % boxes);      // (lane < boxes: its box's rows)
-      if (part && !S::kLatent) {             // values lie block by block, all panels of a block in one box
-        if ((uint32_t)lane < boxes) tma_box(dst + lane * rows_per_box * 128u * S::kBPanels, &map_wide, 0, (int32_t)at, 1, bar);
-      } else if (boxes == 1u) {              // a block (or more) is a tile: the panels in wide boxes, and (MLA) the last one of the scores'
-        if (lane == 0) tma_box(dst, &map_wide, panel_at<S>(part, 0, col0) / 64, (int32_t)at, kv, bar);
-        if (S::kLatent && part == 0 && lane == 0) tma_box(dst + (S::kAPanels - 1) * S::kPanelBytes, &map, S::kDk / 64 - 1, (int32_t)at, 0, bar);
-      } else {                               // a lane for each box of each panel
-        for (uint32_t x0 = 0; x0 < boxes * panels; x0 += 32u) {
-          const uint32_t x = x0 + lane, p = x / boxes, box = x - p * boxes;
-          const uint32_t y = __shfl_sync(~0u, now, first + box);
-          if (x < boxes * panels) tma_box(dst + p * S::kPanelBytes + box * rows_per_box * 128u, &map, panel_at<S>(part, p, col0) / 64, (int32_t)y, kv, bar);
-        }
-      }
-    }
-  } else if (warp < S::kFirst) {
-    // ---- matrix instructions: a warp for each row tile; the whole warp waits, one thread issues ----
-    if (S::kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    const int r = warp - 1;
-    const uint32_t mine = shared ? (n_tiles + 1u - r) / 2u : n_tiles;
-    if (r < teams && mine) {
-      if (S::kDv == S::kCols || col0 == 0) issue<T, S, 0>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, box_rows, status);
-      else issue<T, S, S::kDv - S::kCols>(ctl, tmem, smem_address(q_s), smem_address(ring), r, mine, shared, box_rows, status);
     }
   } else {
     // ---- softmax: a thread per row ----
-    if (S::kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");   // 128 x (72 + 2 x 216) of 384 x 168
+    if (S::kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");   // 128 x (120 + 2 x 192) of 384 x 168
     const int r = (warp - S::kFirst) / 4;
     const uint32_t lane_at = (uint32_t)(warp & 3) * 32u;   // a warp reaches the lanes of its number modulo four
     const uint32_t row = (shared ? 0u : r * 128u) + lane_at + lane;
@@ -639,8 +642,8 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s
   auto* kernel = a.weight ? tiles_kernel<T, S, true> : tiles_kernel<T, S, false>;
   if (S::kTiles == 2) {
     // (the softmax's warps take up registers that the launch has to have given the CTA: fewer, and they would wait for good)
-    static const bool enough[2] = {registers_of(tiles_kernel<T, S, false>) * S::kThreads >= 128 * (72 + 2 * 216),
-                                   registers_of(tiles_kernel<T, S, true>) * S::kThreads >= 128 * (72 + 2 * 216)};
+    static const bool enough[2] = {registers_of(tiles_kernel<T, S, false>) * S::kThreads >= 128 * (120 + 2 * 192),
+                                   registers_of(tiles_kernel<T, S, true>) * S::kThreads >= 128 * (120 + 2 * 192)};
     if (!enough[a.weight ? 1 : 0]) return cudaErrorInvalidConfiguration;
   }
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);

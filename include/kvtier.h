@@ -24,7 +24,8 @@
  *     the library allocates no device memory and never synchronises the device;
  *     GPU work is enqueued on the given streams and results are valid once the
  *     caller has synchronised them.  Use ONE compute stream for every call on a
- *     pool.  kv_demote and kv_promote each take a copy stream; give kv_promote a
+ *     pool, the one that kv_pool_create is given (kv_append and kv_attend may
+ *     be given another, see there).  kv_demote and kv_promote each take a copy stream; give kv_promote a
  *     different one than kv_demote and the H2D copies of a promotion overlap the
  *     D2H copies of the demotion before it (the library orders the two streams
  *     wherever a promotion reads ring slots that a demotion is still writing,
@@ -466,9 +467,11 @@ int32_t kv_dedup_digests(const uint8_t* d_digests, uint64_t m, uint32_t* d_canon
  * d_table (device, u32 [n_rows][n_layers][KV heads]; one column for MLA) holds handles
  * (tags); a run of its rows holds the position-blocks of a sequence, or of a prefix that
  * several share, in order.  A handle leads to its block wherever that is in the partition
- * (d_loc[handle] = entry).  They are enqueued on `stream` (the pool's compute stream),
- * which first joins the pool's promotions in flight; nothing of them waits on the host, and
- * they may be captured into a graph.  q, k, v and outputs may have any strides (elements;
+ * (d_loc[handle] = entry).  They are enqueued on `stream`, which first joins the pool's promotions
+ * in flight; nothing of them waits on the host, and they may be captured into a graph (its replays
+ * join nothing: see kv_join_promotions).  `stream` is the pool's compute stream, or another one that the caller
+ * orders: behind the calls whose work it needs (kv_admit, kv_demote, a kv_append), and the compute stream behind it before
+ * the next call there that changes entries or reads what it has written.  q, k, v and outputs may have any strides (elements;
  * the innermost dimension is contiguous) and the alignment of their elements.  The device
  * that owns the pool has to be the current one. */
 typedef enum { KV_DTYPE_BF16 = 0, KV_DTYPE_F16 = 1 } kv_dtype_t;
@@ -650,6 +653,13 @@ int32_t kv_set_deferred_packing(kv_pool* pool, int32_t on);
  * holds back.  After it returns, synchronising those streams completes the
  * demotion, and d_victims may be reused once they have run.  A no-op otherwise. */
 int32_t kv_flush(kv_pool* pool);
+
+/* Lets `stream` wait for the promotions in flight, behind kv_flush: what every call that reads entries
+ * does for its own stream, on the host, when it is made.  A graph that holds such calls
+ * joins nothing when it is replayed: ahead of a replay behind a kv_promote, call this on the stream of
+ * the replay.  In a stream capture a call is refused (KV_ERR_CUDA; the capture stays valid) while a promotion is
+ * under way that the pool's own stream has not joined, or deferred packing holds something back. */
+int32_t kv_join_promotions(kv_pool* pool, kv_stream_t stream);
 
 /* Largest batch_bytes the staging buffers allow for a partition. */
 uint64_t kv_max_batch_bytes(const kv_pool* pool, int32_t partition);

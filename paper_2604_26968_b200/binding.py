@@ -118,7 +118,7 @@ SLOT_META_DTYPE = np.dtype([("tag", "<u4"), ("last_epoch", "<u4"), ("ema", "<f4"
 EXPORTS = ("kv_size_bytes", "kv_infer_variant", "kv_entry_bytes", "kv_workspace_bytes",
            "kv_pool_create", "kv_pool_destroy", "kv_epoch_score", "kv_epoch_score_select", "kv_epoch_events", "kv_epoch_counts",
            "kv_epoch_update", "kv_set_policy", "kv_set_lazy_decay", "kv_hash_entries", "kv_dedup_table_slots", "kv_dedup_digests", "kv_set_confidence_blend", "kv_reuse_estimate", "kv_head_importance_update", "kv_set_head_multipliers", "kv_head_importance", "kv_head_weights", "kv_prefetch_window_update", "kv_set_prefetch_window", "kv_prefetch_span", "kv_prefetch_window", "kv_prefetch_list", "kv_select_victims", "kv_select_victim_blocks", "kv_select_victims_static", "kv_demote",
-           "kv_promote", "kv_set_deferred_packing", "kv_flush", "kv_max_batch_bytes", "kv_admit", "kv_get_stats", "kv_ring_query",
+           "kv_promote", "kv_set_deferred_packing", "kv_flush", "kv_join_promotions", "kv_max_batch_bytes", "kv_admit", "kv_get_stats", "kv_ring_query",
            "kv_last_demote_counts", "kv_device_status", "kv_timing_enable", "kv_timing_read",
            "kv_set_select_variant", "kv_selection_stats", "kv_demote_counted", "kv_victim_counts", "kv_set_gather_threshold", "kv_set_l2_residency", "kv_last_cuda_error", "kv_status_string",
            "kv_append", "kv_attend", "kv_attend_scratch_bytes", "kv_attention_score",
@@ -207,6 +207,8 @@ def load():
     L.kv_set_deferred_packing.argtypes = [vp, i32]
     L.kv_flush.restype = i32
     L.kv_flush.argtypes = [vp]
+    L.kv_join_promotions.restype = i32
+    L.kv_join_promotions.argtypes = [vp, vp]
     L.kv_max_batch_bytes.restype = u64
     L.kv_max_batch_bytes.argtypes = [vp, i32]
     L.kv_admit.restype = i32
@@ -687,6 +689,9 @@ class Pool:
 
     def kv_flush(self):
         return self.lib.kv_flush(self._h)
+
+    def kv_join_promotions(self, stream=None):
+        return self.lib.kv_join_promotions(self._h, _stream_ptr(stream if stream is not None else self.compute))
 
     def kv_max_batch_bytes(self, partition=0):
         return int(self.lib.kv_max_batch_bytes(self._h, partition))

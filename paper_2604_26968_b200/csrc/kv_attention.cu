@@ -95,6 +95,13 @@ __global__ void __launch_bounds__(kScoreThreads) keep_young_kernel(EntryState st
 
 }  // namespace
 
+bool stream_captured(cudaStream_t s) {
+  cudaStreamCaptureStatus now = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(s, &now) == cudaSuccess) return now != cudaStreamCaptureStatusNone;
+  (void)cudaGetLastError();
+  return true;
+}
+
 cudaError_t launch_attention_score(const EntryState& st, const uint32_t* loc, uint64_t n_tags, uint32_t epoch, float decay, uint32_t protect,
                                    unsigned long long* weight, float* acc, cudaStream_t s) {
   constexpr uint64_t per_cta = kScoreThreads * 4ull;

@@ -121,10 +121,12 @@ struct kv_pool {
   int last_cuda_error = 0;
   ScoreOptions score_opt;   // eviction policy and confidence blend
   uint64_t gather_run_bytes = 1u << 20;    // promote lists whose runs average less go through the gather kernel
-  // promotions run their kernels on the copy stream they are given; the compute stream joins
-  // them (waits for ev_promoted) before the next kernel that reads what they wrote
+  // promotions run their kernels on the copy stream they are given; a call's stream joins
+  // them (waits for ev_promoted) before the next kernel that reads what they wrote.  Open: the pool's
+  // own stream has not joined the last one of the partition yet (another stream's wait is its own affair).
   cudaEvent_t ev_promote_ready, ev_promoted[4];
-  bool promote_open[4] = {false, false, false, false};
+  cudaStream_t own = nullptr;   // the one that kv_pool_create was given
+  bool promoted[4] = {false, false, false, false}, promote_open[4] = {false, false, false, false};
   int select_variant = 1;   // 1 = persistent cooperative selection, 0 = one launch per phase
   PartCounts pc;            // partition bases and where selections leave the victims per partition
   uint32_t* h_sel_stats = nullptr;
@@ -151,6 +153,11 @@ struct kv_pool {
   size_t timed_next = 0;
   kv_timing totals;
 };
+
+namespace kvt {
+// (kv_attention.cu has the answer; the host side built without the kernels takes no stream for a captured one)
+__attribute__((weak)) bool stream_captured(cudaStream_t) { return false; }
+}  // namespace kvt
 
 namespace {
 
@@ -482,23 +489,40 @@ int32_t demote_direct(kv_pool* p) {
     if (rc__ != KV_OK) return rc__;                                         \
   } while (0)
 
+// Nothing can be joined inside a capture: the wait would be for work that the graph does not hold.
+int32_t refuse_capture(kv_pool* p) { return cuda_fail(p, cudaErrorStreamCaptureIsolation); }
+
 // Makes `s` wait for the promotions whose kernels may still be running on their copy streams
-// (all of them, or partition q's only).
+// (all of them, or partition q's only).  The pool's own stream needs one wait for each promotion, any other
+// waits every time: nothing is known of what it has waited for.  A captured stream is refused while a
+// promotion is open, and left alone once the pool's own stream has joined it (the caller replays behind that).
 int32_t join_promotions(kv_pool* p, cudaStream_t s, int q_only = -1) {
+  bool wait[4] = {false, false, false, false}, any = false, open = false;
   for (int q = 0; q < p->n_parts; ++q) {
-    if (!p->promote_open[q] || (q_only >= 0 && q != q_only)) continue;
+    wait[q] = p->promoted[q] && (p->promote_open[q] || s != p->own) && (q_only < 0 || q == q_only);
+    any = any || wait[q];
+    open = open || (wait[q] && p->promote_open[q]);
+  }
+  if (!any) return KV_OK;
+  if (stream_captured(s)) return open ? refuse_capture(p) : KV_OK;
+  for (int q = 0; q < p->n_parts; ++q) {
+    if (!wait[q]) continue;
     KV_CUDA(p, cudaStreamWaitEvent(s, p->ev_promoted[q], 0));
-    p->promote_open[q] = false;
+    if (s == p->own) p->promote_open[q] = false;
   }
   return KV_OK;
 }
 
 // Every call that reads or changes entry state first enqueues what deferred packing holds back
 // and lets its stream wait for the promotions in flight.
+int32_t settle(kv_pool* p, cudaStream_t s) {
+  if (p->pending.active && stream_captured(s)) return refuse_capture(p);   // (a graph would pack again at every replay)
+  KV_DRAIN_ALL(p);
+  return join_promotions(p, s);
+}
 #define KV_SETTLE(pool, stream)                                             \
   do {                                                                      \
-    KV_DRAIN_ALL(pool);                                                     \
-    const int32_t rc2__ = join_promotions(pool, S(stream));                 \
+    const int32_t rc2__ = settle(pool, S(stream));                          \
     if (rc2__ != KV_OK) return rc2__;                                       \
   } while (0)
 
@@ -512,10 +536,7 @@ PoolView pool_view(kv_pool* p) {
   return v;
 }
 
-int32_t pool_settle(kv_pool* p, kv_stream_t stream) {
-  KV_SETTLE(p, stream);
-  return KV_OK;
-}
+int32_t pool_settle(kv_pool* p, kv_stream_t stream) { return settle(p, S(stream)); }
 
 int32_t pool_cuda_error(kv_pool* p, cudaError_t e) { return e == cudaSuccess ? KV_OK : cuda_fail(p, e); }
 
@@ -597,6 +618,7 @@ int32_t kv_pool_create(const kv_pool_desc* desc, kv_stream_t stream, kv_pool** o
   kv_pool* p = new (std::nothrow) kv_pool();
   if (!p) return KV_ERR_INVALID_ARG;
   p->desc = *desc;
+  p->own = S(stream);
   p->n_parts = g.n_parts;
   std::memset(&p->stats, 0, sizeof(p->stats));
   std::memset(&p->totals, 0, sizeof(p->totals));
@@ -1221,7 +1243,7 @@ int32_t kv_promote(kv_pool* p, int32_t q, const uint64_t* h_slots, uint64_t m, u
   if (!listed) KV_CUDA(p, cudaEventRecord(p->ev_list_free[li], copy));
   KV_CUDA(p, cudaEventRecord(p->ev_h2d_done, copy));
   KV_CUDA(p, cudaEventRecord(p->ev_promoted[q], copy));
-  p->promote_open[q] = true;
+  p->promoted[q] = p->promote_open[q] = true;
   p->h2d_valid = true;
   if (gather) p->stats.gathered += m;
   if (p->pending.active) p->pending.promoted[q] += m;
@@ -1353,6 +1375,12 @@ const float* kv_reuse_estimate(kv_pool* p) { return p ? p->ws.blend->estimate : 
 int32_t kv_flush(kv_pool* p) {
   if (!p) return KV_ERR_INVALID_ARG;
   KV_DRAIN_ALL(p);
+  return KV_OK;
+}
+
+int32_t kv_join_promotions(kv_pool* p, kv_stream_t stream) {
+  if (!p) return KV_ERR_INVALID_ARG;
+  KV_SETTLE(p, stream);
   return KV_OK;
 }
 

@@ -33,6 +33,9 @@ inline int sm_count() {
   return n;
 }
 
+// Whether a stream is being captured into a graph; a stream that cannot be asked counts as one that is.
+bool stream_captured(cudaStream_t s);
+
 // Geometry of one partition, as the kernels need it.
 struct PartGeom {
   uint8_t* slab;         // device

@@ -543,7 +543,8 @@ int32_t kv_append(kv_pool* pool, const kv_append_desc* desc, kv_stream_t stream)
  * max_members == 0: no prefix is looked at.
  * d_weight (device, u64 [n_tags], optional): the attention weight p_t of every query head and sequence,
  * summed over the tokens of a block, is added to d_weight[handle], in units of 2^-32 (rounded; integer
- * sums, so that the result does not depend on an order): what kv_attention_score takes.
+ * sums, so that the result does not depend on an order): what kv_attention_score takes.  A query head whose
+ * scores are not numbers (lse is NaN) adds nothing, and takes nothing from what the others add.
  * d_scratch (device, 16-byte aligned): kv_attend_scratch_bytes of the same partition and bounds; two calls
  * that may run at the same time need two.  Same results on every run.
  * head_dim is a multiple of 8 up to 256; MLA: d_latent up to 512 and d_latent + d_rope up to 576, multiples

@@ -611,12 +611,10 @@ __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_con
       for (uint32_t r = row0 + lane; r < rows; r += lanes) {
         const uint32_t member = a.by_group(r);
         const float lse = total[(uint64_t)(seq0 + member) * a.q_heads + head * a.group + (r - member * a.group)];
-        if (lse == -INFINITY) continue;
+        if (!(fabsf(lse) < INFINITY)) continue;      // a row with nothing to attend to, or whose scores are no numbers: the others count
         for (uint32_t g = g0; g < g1; ++g) sum += exp2_(grain[(uint64_t)g * stride + r] - lse);
       }
-      // in units of 2^-32; NaN counts as nothing
-      const float x = sum * 0x1p32f;
-      w = x > 0.0f ? __float2ull_rn(fminf(x, 0x1p62f)) : 0ull;
+      w = __float2ull_rn(fminf(sum * 0x1p32f, 0x1p62f));      // in units of 2^-32
     }
   } else {
     wait_for_kernel_ahead();

@@ -571,7 +571,8 @@ typedef struct {
   uint64_t scratch_bytes;
 } kv_attend_desc;
 int32_t kv_attend(kv_pool* pool, const kv_attend_desc* desc, kv_stream_t stream);
-/* Scratch of a call with these bounds (weights: with d_weight); 0 if kv_attend would refuse them. */
+/* Scratch of a call with these bounds (weights: with d_weight); 0 if kv_attend would refuse them: more work than
+ * launches can take (2^31 - 1 CTAs, blocks to weigh times 256 query rows below 0xf0000000) or parts beyond 2^46 bytes. */
 uint64_t kv_attend_scratch_bytes(kv_pool* pool, int32_t partition, uint32_t n_seqs, uint32_t n_groups,
                                  uint32_t max_suffix, uint32_t max_prefix, uint32_t max_members, int32_t weights);
 

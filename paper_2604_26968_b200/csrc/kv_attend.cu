@@ -467,8 +467,7 @@ __global__ void __launch_bounds__(kM * kN * 32) latent_kernel(const __grid_const
 
 // ---- parts to outputs, grains to weights -------------------------------------------------------------
 
-constexpr int kFinishThreads = 256, kFinishRows = kFinishThreads / 32;
-constexpr uint32_t kWeightRows = 256;
+constexpr int kFinishRows = kFinishThreads / 32;
 
 // The parts of a sequence: np of its group's prefix, ns of its suffix, the latter behind the places of all prefix chunks.
 struct Parts {
@@ -573,7 +572,7 @@ __global__ void __launch_bounds__(kFinishThreads) weight_kernel(const __grid_con
                                                                uint32_t suffix_shift) {
   const int kind = blockIdx.x < prefix_ctas ? kKindPrefix : kKindSuffix;
   const uint32_t shift = kind == kKindPrefix ? prefix_shift : suffix_shift, lanes = 1u << shift;
-  // (fewer than 2^32 items, see the launch: 64-bit divisions were most of this kernel's time)
+  // (fewer than 2^32 items, kMaxWeightItems: 64-bit divisions were most of this kernel's time)
   const uint32_t item = (blockIdx.x - (kind == kKindPrefix ? 0u : prefix_ctas)) * (kFinishThreads >> shift) + (threadIdx.x >> shift);
   const uint32_t lane = threadIdx.x & (lanes - 1u);
   const uint32_t most_blocks = ((kind == kKindPrefix ? a.max_prefix : a.max_suffix) + a.tv.block_tokens - 1u) / a.tv.block_tokens;
@@ -632,7 +631,6 @@ cudaError_t launch_items(F* kernel, unsigned threads, size_t smem, const AttendA
   const uint64_t np = prefix ? (rows + row_tile_prefix - 1) / row_tile_prefix * a.chunks[0] * a.tv.heads * a.n_groups : 0;
   const uint64_t ns = suffix ? (a.group + row_tile_suffix - 1) / row_tile_suffix * (uint64_t)a.chunks[1] * a.tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
-  if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   return launch_overlapped_smem(kernel, (unsigned)(np + ns), threads, smem, s, a, (uint32_t)np);
@@ -697,13 +695,11 @@ cudaError_t launch_typed(const AttendArgs& a, int dtype, bool mla, cudaStream_t 
     const uint32_t most = kind == kKindPrefix ? a.max_prefix : a.max_suffix;
     const uint64_t blocks = ((uint64_t)most + a.tv.block_tokens - 1u) / a.tv.block_tokens;
     const uint32_t r = kind == kKindPrefix ? a.max_members * a.group : a.group;
-    while (shift[kind] < 5u && (1u << shift[kind]) < r) ++shift[kind];
+    shift[kind] = weight_shift(r);
     const uint64_t items = (uint64_t)(kind == kKindPrefix ? a.n_groups : a.n_seqs) * a.tv.heads * blocks * ((r + kWeightRows - 1u) / kWeightRows);
-    if (items > 0xf0000000ull) return cudaErrorInvalidValue;
     ctas[kind] = ((items << shift[kind]) + kFinishThreads - 1) / kFinishThreads;
   }
   if (ctas[0] + ctas[1] == 0) return cudaSuccess;
-  if (ctas[0] + ctas[1] > 0x7fffffffull) return cudaErrorInvalidValue;
   return launch_overlapped(weight_kernel, (unsigned)(ctas[0] + ctas[1]), (unsigned)kFinishThreads, s, a, (uint32_t)ctas[0], shift[0], shift[1]);
 }
 

@@ -124,7 +124,17 @@ struct AttendArgs {
 
 constexpr uint32_t kMaxRowDim = 576;          // widest row of keys (MLA)
 constexpr uint32_t kStreamUnit = 16, kStreamTokens = 1024;   // a warp's of kv_attend_stream.cu
+constexpr int kFinishThreads = 256;           // of a CTA that joins parts or adds weights up
+constexpr uint32_t kWeightRows = 256;         // rows of a block that one item of the weights takes
+constexpr uint64_t kMaxGrid = 0x7fffffffull, kMaxWeightItems = 0xf0000000ull;   // of a launch: a call beyond them is refused (split)
 constexpr uint32_t kMaxChunkTokens = 4096, kMaxChunkBlocks = 256;   // most a CTA takes of a segment
+
+// log2 of the threads that add up a block's weight of so many rows
+inline uint32_t weight_shift(uint32_t rows) {
+  uint32_t shift = 0;
+  while (shift < 5u && (1u << shift) < rows) ++shift;
+  return shift;
+}
 
 // kv_attend.cu
 cudaError_t launch_attend(const AttendArgs& a, int dtype, bool mla, cudaStream_t s);

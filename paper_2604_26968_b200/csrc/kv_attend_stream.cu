@@ -273,7 +273,6 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, bool behind_ti
   const uint64_t np = prefix ? ((uint64_t)a.max_members * a.group + 15) / 16 * a.chunks[0] * tv.heads * a.n_groups : 0;
   const uint64_t ns = suffix ? (a.group + 15) / 16 * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   if (np + ns == 0) return cudaSuccess;
-  if (np + ns > 0x7fffffffull) return cudaErrorInvalidValue;
   auto* kernel = a.weight ? stream_kernel<T, D, true> : stream_kernel<T, D, false>;
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::kSmem);
   if (e != cudaSuccess) return e;

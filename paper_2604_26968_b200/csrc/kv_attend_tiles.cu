@@ -638,7 +638,6 @@ cudaError_t launch(const AttendArgs& a, bool prefix, bool suffix, cudaStream_t s
   const uint64_t ns = suffix ? (a.group + tile - 1) / tile * (uint64_t)a.chunks[1] * tv.heads * a.n_seqs : 0;
   const uint64_t grid = (np + ns) * (S::kDv / S::kCols);
   if (grid == 0) return cudaSuccess;
-  if (grid > 0x7fffffffull) return cudaErrorInvalidValue;
   auto* kernel = a.weight ? tiles_kernel<T, S, true> : tiles_kernel<T, S, false>;
   if (S::kTiles == 2) {
     // (the softmax's warps take up registers that the launch has to have given the CTA: fewer, and they would wait for good)

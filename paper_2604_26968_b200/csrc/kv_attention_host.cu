@@ -152,6 +152,20 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
       out->chunks[k] = (uint32_t)c[k].chunks();
     }
   }
+  // what the launches will be: nothing is enqueued of a call that one of them could not take
+  typedef unsigned __int128 Count;
+  Count by_tiles = 0, by_streams = 0, by_rest = 0, weight_ctas = 0;
+  for (int k = shared ? 0 : 1; k < 2; ++k) {
+    const uint64_t segs = (uint64_t)(k == 0 ? n_groups : n_seqs) * heads, kind_rows = k == 0 ? prefix_rows : group;
+    if (out->tiles[k]) by_tiles += (Count)tiles[k].ctas * out->chunks[k];
+    else if (out->stream[k]) by_streams += (Count)((kind_rows + 15) / 16) * segs * out->chunks[k];
+    else by_rest += (Count)rest[k].ctas * out->chunks[k];
+    if (!weights) continue;
+    const Count items = (Count)segs * (((uint64_t)(k == 0 ? max_prefix : max_suffix) + bt - 1) / bt) * ((kind_rows + kWeightRows - 1) / kWeightRows);
+    if (items > kMaxWeightItems) return false;
+    weight_ctas += (items << weight_shift((uint32_t)kind_rows)) / kFinishThreads + 1;
+  }
+  if (by_tiles > kMaxGrid || by_streams > kMaxGrid || by_rest > kMaxGrid || weight_ctas > kMaxGrid) return false;
   out->n_parts = out->chunks[0] * out->per_chunk[0] + out->chunks[1] * out->per_chunk[1];
   out->grain_tokens = bt % 16 == 0 ? 16 : 1;
   const unsigned __int128 rows = (unsigned __int128)n_seqs * q_heads;

@@ -582,7 +582,7 @@ uint64_t kv_attend_scratch_bytes(kv_pool* pool, int32_t partition, uint32_t n_se
  *   d_score[entry] = d_acc[g], or +inf if fewer than `protect` epochs lie between the entry's last
  *                    epoch (its last touch, or its admission) and `epoch`;
  * FREE entries get +inf.  kv_select_victims (or kv_select_victim_blocks) then chooses the lowest.
- * d_weight (device, u64 [n_tags]) and d_acc (device, f32 [n_tags]) are zeroed by the caller once; they
+ * d_weight (device, u64 [n_tags]) and d_acc (device, f32 [n_tags]), NULL in a pool without handles, are zeroed by the caller once; they
  * belong to handles, so a block keeps what it has gathered while it is in the host tier, where it does not decay.
  * Handles are gone through by d_loc; a caller that has led a second handle to an entry gets the score of either.
  * 0 <= decay <= 1; protect < 2^31, 0: no entry is young.  The pool's predictor, EMA and touches are left alone. */

@@ -106,7 +106,9 @@ cudaError_t launch_attention_score(const EntryState& st, const uint32_t* loc, ui
                                    unsigned long long* weight, float* acc, cudaStream_t s) {
   constexpr uint64_t per_cta = kScoreThreads * 4ull;
   if (n_tags > KV_NONE) n_tags = KV_NONE;
-  const cudaError_t e = launch_overlapped(fold_weights_kernel, (unsigned)((n_tags + per_cta - 1u) / per_cta), (unsigned)kScoreThreads, s, st.score,
+  // (a pool without handles: one CTA that finds nothing, as the kernel behind counts on one between itself and all that came before)
+  const uint64_t fold_ctas = n_tags ? (n_tags + per_cta - 1u) / per_cta : 1u;
+  const cudaError_t e = launch_overlapped(fold_weights_kernel, (unsigned)fold_ctas, (unsigned)kScoreThreads, s, st.score,
                                           st.n, loc, n_tags, decay, weight, acc);
   if (e != cudaSuccess) return e;
   return launch_overlapped(keep_young_kernel, (unsigned)((st.n + per_cta - 1u) / per_cta), (unsigned)kScoreThreads, s, st, epoch, (int32_t)protect);

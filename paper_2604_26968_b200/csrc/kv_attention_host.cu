@@ -329,10 +329,11 @@ int32_t kv_append(kv_pool* p, const kv_append_desc* d, kv_stream_t stream) {
 int32_t kv_attention_score(kv_pool* p, uint32_t epoch, float decay, uint32_t protect, uint64_t* d_weight, float* d_acc,
                            kv_stream_t stream) {
   if (!p || !(decay >= 0.0f && decay <= 1.0f) || protect >= 0x80000000u) return KV_ERR_INVALID_ARG;
-  if (!d_weight || !d_acc || !aligned(d_weight, 16) || !aligned(d_acc, 16)) return KV_ERR_INVALID_ARG;
+  const PoolView v = pool_view(p);
+  if (v.desc->n_tags && (!d_weight || !d_acc)) return KV_ERR_INVALID_ARG;
+  if (!aligned(d_weight, 16) || !aligned(d_acc, 16)) return KV_ERR_INVALID_ARG;
   const int32_t rs = pool_settle(p, stream);
   if (rs != KV_OK) return rs;
-  const PoolView v = pool_view(p);
   return pool_cuda_error(p, launch_attention_score(v.st, v.desc->d_loc, v.desc->n_tags, epoch, decay, protect,
                                                    reinterpret_cast<unsigned long long*>(d_weight), d_acc, S(stream)));
 }

@@ -584,7 +584,11 @@ uint64_t kv_attend_scratch_bytes(kv_pool* pool, int32_t partition, uint32_t n_se
  * FREE entries get +inf.  kv_select_victims (or kv_select_victim_blocks) then chooses the lowest.
  * d_weight (device, u64 [n_tags]) and d_acc (device, f32 [n_tags]), NULL in a pool without handles, are zeroed by the caller once; they
  * belong to handles, so a block keeps what it has gathered while it is in the host tier, where it does not decay.
- * Handles are gone through by d_loc; a caller that has led a second handle to an entry gets the score of either.
+ * Handles are gone through by d_loc, which may lead no second handle to an entry (demotion would move the entry's own alone):
+ * a block that several sequences share has its one handle in all of their tables, and gathers all of their weight there.
+ * An entry's last epoch follows touches (at a scoring pass) and admission, not kv_append or kv_attend: an engine that evicts by attention
+ * weight alone writes d_last_epoch of the blocks that it is still filling itself, on the compute stream.  Otherwise such a block is young for
+ * `protect` epochs only, has little weight, and may be evicted; the next kv_append into it is then left out (KV_DEV_BLOCK_NOT_RESIDENT).
  * 0 <= decay <= 1; protect < 2^31, 0: no entry is young.  The pool's predictor, EMA and touches are left alone. */
 int32_t kv_attention_score(kv_pool* pool, uint32_t epoch, float decay, uint32_t protect, uint64_t* d_weight,
                            float* d_acc, kv_stream_t stream);

@@ -552,7 +552,7 @@ int32_t kv_append(kv_pool* pool, const kv_append_desc* desc, kv_stream_t stream)
 typedef struct {
   int32_t partition, layer;
   int32_t dtype;           /* kv_dtype_t */
-  float scale;
+  float scale;             /* finite, as is scale / log 2 */
   uint32_t n_seqs, n_groups;
   uint32_t max_suffix, max_prefix, max_members;
   uint32_t reserved;

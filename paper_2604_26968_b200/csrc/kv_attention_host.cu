@@ -215,7 +215,8 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   const int32_t rc = dims(v, q, &dk, &dv);
   if (rc != KV_OK) return rc;
   if (!attend_dims(v, q, dk, dv)) return KV_ERR_UNSUPPORTED_VARIANT;
-  if (!std::isfinite(d->scale)) return KV_ERR_INVALID_ARG;
+  const float scale2 = d->scale * 1.44269504088896340736f;   // exponentials are of base 2
+  if (!std::isfinite(scale2)) return KV_ERR_INVALID_ARG;
   if (d->n_seqs == 0) return KV_OK;
   if (!d->d_q || !d->d_out || !aligned(d->d_q, 2) || !aligned(d->d_out, 2) || !d->d_suffix || !aligned(d->d_suffix, 4)) return KV_ERR_INVALID_ARG;
   if (d->n_groups && (!d->d_prefix || !d->d_group || !aligned(d->d_prefix, 4) || !aligned(d->d_group, 4))) return KV_ERR_INVALID_ARG;
@@ -235,7 +236,7 @@ int32_t kv_attend(kv_pool* p, const kv_attend_desc* d, kv_stream_t stream) {
   a.q_head = d->q_stride[1];
   a.out_seq = d->out_stride[0];
   a.out_head = d->out_stride[1];
-  a.scale2 = d->scale * 1.44269504088896340736f;
+  a.scale2 = scale2;
   a.n_seqs = d->n_seqs;
   a.n_groups = sp.chunks[0] ? d->n_groups : 0u;
   a.q_heads = (uint32_t)v.desc->part[q].model.n_q_heads;

@@ -55,10 +55,10 @@ static kv_pool* make(const kv_model_desc& m, int block_tokens) {
 
 struct Bounds { uint32_t seqs, groups, suffix, prefix, members; int weights; };
 static void* g_mem;
-static int32_t call(kv_pool* p, const Bounds& b, uint64_t scratch) {
+static int32_t call(kv_pool* p, const Bounds& b, uint64_t scratch, float scale = 0.125f) {
   kv_attend_desc a{};
   a.dtype = KV_DTYPE_BF16;
-  a.scale = 0.125f;
+  a.scale = scale;
   a.n_seqs = b.seqs;
   a.n_groups = b.groups;
   a.max_suffix = b.suffix;
@@ -118,6 +118,11 @@ int main() {
   g_tiles = g_streams = false;
   refused(mha, {1, 1u << 23, 16, 1u << 20, 1, 0}, "the same, by rows");
   refused(mla, {1, 1u << 23, 16, 1u << 28, 1, 0}, "the same, latent rows");
+  // a scale that is finite, but not by 1 / log 2
+  const Bounds one{1, 0, 16, 0, 0, 0};
+  expect(call(mha, one, ~0ull, 2e38f) == KV_OK && call(mha, one, ~0ull, -2e38f) == KV_OK, "a large scale");
+  const int before_scale = g_attend;
+  expect(call(mha, one, ~0ull, 3e38f) == KV_ERR_INVALID_ARG && call(mha, one, ~0ull, -3e38f) == KV_ERR_INVALID_ARG && g_attend == before_scale, "too large a scale");
   // whatever is taken fits
   std::mt19937_64 rng(5);
   int took = 0, not_taken = 0;

@@ -32,11 +32,12 @@ struct Vec<T, 1> {
   T x[1];
 };
 
-// cos and sin of pos * freq
+// cos and sin of pos * freq, the product rounded to 64 bits and reduced by 2 pi in two parts (the first alone would leave 4e-17 of the
+// angle: 8e-5 rad at 2 10^12)
 __device__ __forceinline__ float2 turn(int32_t pos, float freq) {
-  const double a = __dmul_rn((double)pos, (double)freq);   // exact: 31 + 24 bits are at most two too many
+  const double a = __dmul_rn((double)pos, (double)freq);
   const double k = rint(__dmul_rn(a, 0.15915494309189533577));
-  const float r = (float)__fma_rn(-k, 6.283185307179586477, a);
+  const float r = (float)__fma_rn(-k, 2.4492935982947064e-16, __fma_rn(-k, 6.283185307179586477, a));
   float2 cs;
   sincosf(r, &cs.y, &cs.x);
   return cs;

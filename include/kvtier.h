@@ -498,7 +498,8 @@ typedef struct {
  * other's.  A head whose block is not in HBM is left out and sets KV_DEV_BLOCK_NOT_RESIDENT; a
  * slot beyond the table sets KV_DEV_BAD_INDEX and nothing of its token is written.
  * A key head has head_dim elements (MLA: one row of d_latent + d_rope elements, and no values:
- * d_v is NULL); so has a query head.  Results are rounded once from binary32. */
+ * d_v is NULL); so has a query head.  Results are rounded once from binary32.  A token of 2^31 elements or more is not
+ * taken (KV_ERR_UNSUPPORTED_VARIANT). */
 typedef struct {
   int32_t partition, layer;
   int32_t dtype;           /* kv_dtype_t */

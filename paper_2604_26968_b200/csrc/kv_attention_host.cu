@@ -294,6 +294,9 @@ int32_t kv_append(kv_pool* p, const kv_append_desc* d, kv_stream_t stream) {
   if (d->n_tokens > 0x7fffffffull || d->n_rows >= 0x100000000ull) return KV_ERR_INVALID_ARG;
   if (!d->d_k || !aligned(d->d_k, 2) || (mla ? d->d_v != nullptr : !d->d_v) || !aligned(d->d_v, 2)) return KV_ERR_INVALID_ARG;
   if ((d->d_q != nullptr) != (d->d_q_out != nullptr) || !aligned(d->d_q, 2) || !aligned(d->d_q_out, 2)) return KV_ERR_INVALID_ARG;
+  // (a token's elements are counted in 31 bits)
+  const uint64_t heads = v.geom[q].heads, q_heads = d->d_q ? (uint64_t)v.desc->part[q].model.n_q_heads : 0u;
+  if ((heads + q_heads) * dk + (mla ? 0u : heads * dv) >= 0x80000000ull) return KV_ERR_UNSUPPORTED_VARIANT;
   if (!d->d_slot || !aligned(d->d_slot, 8) || (d->n_rows && (!d->d_table || !aligned(d->d_table, 4)))) return KV_ERR_INVALID_ARG;
   const int32_t rs = pool_settle(p, stream);
   if (rs != KV_OK) return rs;

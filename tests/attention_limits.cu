@@ -123,6 +123,22 @@ int main() {
   expect(call(mha, one, ~0ull, 2e38f) == KV_OK && call(mha, one, ~0ull, -2e38f) == KV_OK, "a large scale");
   const int before_scale = g_attend;
   expect(call(mha, one, ~0ull, 3e38f) == KV_ERR_INVALID_ARG && call(mha, one, ~0ull, -3e38f) == KV_ERR_INVALID_ARG && g_attend == before_scale, "too large a scale");
+  // tokens of 2^31 elements and more: queries of 2^22 latent heads
+  kv_pool* const broad = make(kv_model_desc{KV_MLA, 2, 1 << 22, 1 << 22, 128, 512, 64, 16}, 64);
+  if (!broad) return fail("pool of many heads");
+  kv_append_desc t{};
+  t.dtype = KV_DTYPE_BF16;
+  t.n_tokens = 3;
+  t.d_k = t.d_q = t.d_q_out = g_mem;
+  t.d_table = (const uint32_t*)g_mem;
+  t.n_rows = 20;
+  t.d_slot = (const int64_t*)g_mem;
+  expect(kv_append(broad, &t, (void*)1) == KV_ERR_UNSUPPORTED_VARIANT, "tokens of 2^31 elements");
+  t.d_q = t.d_q_out = nullptr;
+  expect(kv_append(broad, &t, (void*)1) == KV_OK, "their keys alone");
+  t.d_q = t.d_q_out = g_mem;
+  expect(kv_append(mla, &t, (void*)1) == KV_OK, "tokens of ordinary heads");
+  kv_pool_destroy(broad);
   // whatever is taken fits
   std::mt19937_64 rng(5);
   int took = 0, not_taken = 0;

@@ -29,8 +29,10 @@ constexpr int kTile = 64;   // tokens of a tile
 // shared memory in kStages stages filled by cp.async, 16-byte chunks of a row exchanged by row & 7, which
 // keeps ldmatrix free of bank conflicts.  Tokens that are not there are zeros in both tiles and -inf in the
 // scores, so nothing of what lies in such places reaches a sum.
-// Few rows (a suffix) are bound by HBM: the matrix instructions then run mostly empty, at about a fifth of
-// their rate.
+// What comes here: rows of other than 64 or 128 elements, blocks of other than 16 n tokens (and blocks that no tile is made of, by
+// 33 rows or more).  64 runs of up to 1,500 tokens: heads of 96, 4 rows, 78 us (0.35 of the bytes' time); heads of 256, 4 rows, 110 us (0.33);
+// blocks of 8 tokens 81 us (0.45).  Where many rows read a block, the products bound it: a prefix of 8,000 tokens by 256 rows a head of 256
+// 159 us, by blocks of 8 173 us (0.08 of the bytes' time).
 template <typename T, int D, int kM, int kN, int kStages>
 __global__ void __launch_bounds__(kM * kN * 32) rows_kernel(const __grid_constant__ AttendArgs a, uint32_t first_kind_items) {
   constexpr int kWarps = kM * kN, kThreadsHere = kWarps * 32;

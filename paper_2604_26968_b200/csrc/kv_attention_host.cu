@@ -60,8 +60,8 @@ struct Cut {
   uint64_t chunks() const { return ctas ? (tiles + per - 1) / per : 0; }
 };
 // The cuts of prefixes and suffixes that one launch runs through, `slots` CTAs at a time, prefixes first: those for which the
-// longer of the longest CTA and an even share of all of them is shortest.  A CTA costs `extra` tiles beside its own; suffixes
-// are taken to be as long as their bound for six parts in ten; a part more than one in all costs another launch.
+// longer of the longest CTA and an even share of all of them is shortest.  A CTA costs `extra` tiles beside its own; runs
+// are taken to be as long as their bounds; a part more than one in all costs another launch.
 void cut(Cut& p, Cut& s, uint64_t slots, uint64_t extra, bool alone) {
   uint64_t best = ~0ull, best_p = 1, best_s = 1;
   auto first = [](const Cut& c) { return c.ctas ? (c.tiles + c.most_per - 1) / c.most_per : 1; };
@@ -77,7 +77,7 @@ void cut(Cut& p, Cut& s, uint64_t slots, uint64_t extra, bool alone) {
       if (!n_p || !n_s) {
         cost = (n_p + n_s + slots - 1) / slots * (longest + extra);
       } else {
-        const uint64_t all = n_p * (p.per + extra) + s.ctas * (s.tiles * 6 / 10) + n_s * extra;
+        const uint64_t all = n_p * (p.per + extra) + s.ctas * s.tiles + n_s * extra;
         cost = all / slots + (n_p + n_s > slots ? ((p.per < s.per ? p.per : s.per) + extra) / 2 : 0);
         if (cost < longest + extra) cost = longest + extra;
       }
@@ -130,7 +130,8 @@ bool split(const PoolView& v, int32_t q, uint32_t dk, uint32_t dv, uint32_t n_se
       out->per_chunk[k] = !mla && rows <= 128 ? 2 : 1;
       tiles[k] = Cut{(rows + tile - 1) / tile * segs * (mla ? 2 : 1), ((uint64_t)most + 63) / 64, limit / 64, 1};
     } else if (out->stream[k]) {
-      // a warp's chunk: enough of them for all warps if runs are as long as these bounds for six parts in ten, 8 to 32 units
+      // a warp's chunk, 8 to 32 units: chunks for five warps in six where all runs are as long as their bound.  (0.6 as many: MQA of ragged
+      // runs 36 -> 42 us, of one long run among short ones 29 -> 33, of equal runs 42 -> 41; MHA with one long run 55 -> 43, else even.)
       const uint64_t units = ((uint64_t)most + kStreamUnit - 1) / kStreamUnit;
       uint64_t per = (rows + 15) / 16 * segs * units * 12 / 10 / (kSms * stream_warps(dk));
       per = per < 8 ? 8 : per > 32 ? 32 : per;

@@ -540,7 +540,8 @@ int32_t kv_append(kv_pool* pool, const kv_append_desc* desc, kv_stream_t stream)
  * values in the elements' type.
  * max_suffix, max_prefix (tokens) and max_members (sequences of a group) bound what the arrays hold:
  * the arrays may change between replays of a captured call, the bounds may not.  A run or group
- * beyond them or beyond the table counts as empty and sets KV_DEV_BAD_INDEX.  max_prefix == 0 or
+ * beyond them or beyond the table counts as empty and sets KV_DEV_BAD_INDEX.  Scratch and launches are laid out by the bounds: 64
+ * runs of up to 1,500 tokens that take 69 us under a bound of 1,500 take 76 under 8,192 and 191 under 131,072.  max_prefix == 0 or
  * max_members == 0: no prefix is looked at.
  * d_weight (device, u64 [n_tags], optional): the attention weight p_t of every query head and sequence,
  * summed over the tokens of a block, is added to d_weight[handle], in units of 2^-32 (rounded; integer

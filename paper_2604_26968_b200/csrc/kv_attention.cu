@@ -7,7 +7,7 @@
 // Bound: HBM.  Handles go in order, a thread for four of them: block table, weights and accumulators (28 bytes a handle)
 // are streamed, and only the score (4 bytes) is reached through the table.  A second launch goes over the entries in order and
 // overwrites the scores of those that are FREE or young.  Where no two neighbouring entries have neighbouring handles
-// (18.8 M entries): 225 + 26 us; entries in order, weights and accumulators reached by handle, 1,186; the last epoch and the
+// (18.8 M entries): 262 us for both, 310 with weight in every entry and nothing in the L2; entries in order, weights and accumulators reached by handle, 1,186; the last epoch and the
 // entry's own handle reached through the table as well, 1,040.  3.1 M entries with handles in runs of eight: 16 + 6 us.
 #include "kv_attend.cuh"
 
